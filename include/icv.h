@@ -16,8 +16,8 @@
  *    Calls enqueue work on it and return without synchronising.
  *  - Return value: ICV_OK or a negative icv_status; nothing aborts or throws.
  *    Invalid arguments are detected on the host before anything is launched.
- *  - Base pointers must be 16-byte aligned.  Pixel strides are free; the fastest
- *    kernels want rows of whole 32- or 64-byte units at 16-byte multiples.
+ *  - Base pointers must be 16-byte aligned (the sequence and 8-bit operators at the end name their own exceptions).
+ *    Pixel strides are free; the fastest kernels want rows of whole 32- or 64-byte units at 16-byte multiples.
  */
 #ifndef ICV_H
 #define ICV_H
@@ -248,6 +248,147 @@ ICV_API int icv_conv2d_nhwc_im2col(const icv_conv_params* p, const void* input, 
 ICV_API size_t icv_static_workspace_bytes(void);
 ICV_API int icv_conv2d_nhwc_im2col_static(const icv_conv_params* p, const void* input, const void* packed_filter,
                                   void* output, void* stream);
+
+/*
+ * ======== Operators on sequences: the short causal convolution and the selective scan behind it ========
+ *
+ * Layers that mix along a sequence instead of over an image: a depthwise convolution of a few taps that looks back
+ * only, and a linear recurrence whose coefficients come from the input.  Tensors are rows of channels, channels
+ * innermost, like the NHWC tensors above with one pixel per token; rows may be strided (row strides in elements, 0
+ * means dense), so that a slice of a wider matrix is taken as it lies.  Data pointers need only their element's
+ * alignment.  Types: ICV_F32 or ICV_BF16 for the rows; states of the scan, its coefficients and all sums are float.
+ *
+ * icv_sequences says which of the `tokens` rows belong to which sequence and where the sequences' states are kept.
+ * The struct is host memory; the arrays it points to are int32 DEVICE memory, each may be NULL, and they are read when
+ * the kernels run, so a captured graph follows what they then hold.
+ *   start  : count + 1 entries, non-decreasing, 0..tokens: sequence i has the rows start[i] .. start[i + 1] - 1.
+ *            NULL: every sequence has tokens / count rows (which must divide)
+ *   length : count entries: only the first length[i] of these rows belong to the sequence (a padded batch; values
+ *            outside 0..its rows count as the nearer bound).  NULL: all of them
+ *   from   : count entries: the state slot the sequence continues; a value outside 0..slots-1 starts it from zeros.
+ *            NULL: slot i
+ *   to     : count entries: the slot that takes the state behind the sequence's last row; a value outside 0..slots-1:
+ *            it is not kept.  NULL: slot i
+ * Rows of no sequence are neither read nor written.  A sequence of no rows leaves every slot as it is.  Start values
+ * outside 0..tokens are taken as the nearer bound and never lead out of the tensors; where they decrease, which rows are computed is
+ * undefined.  A slot may be continued by several sequences; a slot that a sequence writes must not be read or written
+ * by another one of the same call (reading and writing the same slot by one sequence is the usual case).
+ * One new token per sequence is tokens == count without `start`.
+ * count = 0 or tokens = 0: nothing to do, ICV_OK.
+ */
+typedef struct icv_sequences {
+    int32_t count;
+    int32_t tokens;
+    const int32_t* start;
+    const int32_t* length;
+    const int32_t* from;
+    const int32_t* to;
+} icv_sequences;
+
+/*
+ * Short causal convolution of every channel d along its sequence, t counted in the sequence:
+ *   y[t][d] = act(bias[d] + sum_k filter[d][k] * x[t - (taps-1) + k][d]),  act(v) = v, or v / (1 + exp(-v)) with silu,
+ * sums in float, one rounding at the store.  Rows in front of the first are the taps-1 rows of the state (oldest
+ * first); the state behind a sequence is the last taps-1 rows of the old state and the sequence's own.
+ *   input  : [tokens] rows of in_row_stride elements (first `channels` used)
+ *   filter : [channels][taps], of the rows' type (Listing 1's filter for one channel in and out), bias: channels floats or NULL
+ *   state  : [state_slots] slots of state_slot_stride elements, [taps-1][channels] used, of the rows' type; NULL: all
+ *            sequences start from zeros and no state is kept
+ *   output : [tokens] rows of out_row_stride elements of the rows' type; must not be the input
+ */
+typedef struct icv_causal_conv_params {
+    int32_t channels, taps;         /* taps 1..8 */
+    int32_t in_row_stride, out_row_stride;
+    int32_t dtype;                  /* ICV_F32 or ICV_BF16 */
+    int32_t silu;                   /* 0 or 1 */
+    int32_t state_slots;
+    int64_t state_slot_stride;      /* 0 means (taps-1) * channels */
+} icv_causal_conv_params;
+ICV_API int icv_causal_conv1d(const icv_causal_conv_params* p, const icv_sequences* seq, const void* input,
+                              const void* filter, const float* bias, void* state, void* output, void* stream);
+
+/*
+ * Selective state space scan.  Channel d has `states` state values; the channels are divided into `groups` equal runs
+ * that share B and C.  Per row t of a sequence, g = d / (channels / groups):
+ *   delta = dt[t][d] + dt_bias[d], through log(1 + exp(.)) with softplus
+ *   h[d][n] = exp(delta * A[d][n]) * h[d][n] + delta * x[t][d] * B[t][g][n]
+ *   y[t][d] = sum_n C[t][g][n] * h[d][n] + D[d] * x[t][d],  times z / (1 + exp(-z)) of z[t][d] where z is given
+ * All in float (states, decays, sums); y is rounded once, at the store.
+ *   x, dt, z, out : [tokens] rows of channels; z may be NULL.  out may be x, dt or z where the row strides agree
+ *   B, C          : [tokens] rows of groups * states
+ *   A             : [channels][states] float; D, dt_bias: channels floats, or NULL
+ *   state         : [state_slots] slots of state_slot_stride floats, [channels][states] used; NULL: all sequences
+ *                   start from zeros and no state is kept
+ * workspace: icv_selective_scan_workspace_bytes() bytes of device memory, 16-byte aligned (long sequences of few
+ * channels are cut into pieces whose states meet there); NULL where that is 0.  Nothing in it need be cleared or is
+ * kept; calls that may overlap in time need one each.
+ */
+typedef struct icv_scan_params {
+    int32_t channels, states, groups;   /* states 1..64 (more: ICV_ERR_UNSUPPORTED); groups divides channels */
+    int32_t x_row_stride, dt_row_stride, b_row_stride, c_row_stride, z_row_stride, out_row_stride;
+    int32_t dtype;                      /* ICV_F32 or ICV_BF16: x, dt, B, C, z, out */
+    int32_t softplus;                   /* 0 or 1 */
+    int32_t state_slots;
+    int64_t state_slot_stride;          /* 0 means channels * states */
+} icv_scan_params;
+typedef struct icv_scan_tensors {
+    const void* x;
+    const void* dt;
+    const float* A;
+    const void* B;
+    const void* C;
+    const float* D;
+    const void* z;
+    const float* dt_bias;
+    float* state;
+    void* out;
+} icv_scan_tensors;
+ICV_API size_t icv_selective_scan_workspace_bytes(const icv_scan_params* p, const icv_sequences* seq);
+ICV_API int icv_selective_scan(const icv_scan_params* p, const icv_sequences* seq, const icv_scan_tensors* tensors,
+                               void* workspace, void* stream);
+
+/*
+ * ======== Matrix product in 8-bit floating point with a scale per block of 128 ========
+ *
+ * A matrix in e4m3 (4 exponent, 3 mantissa bits, no infinities, largest value 448): rows of codes, row stride a
+ * multiple of 16 bytes, each row continued with zero codes to a whole multiple of 128, and one float per block of
+ * 128 columns and block_rows rows, stored [column block][row block].  An element is code * scale.
+ * icv_quantize_fp8 makes this form from rows of ICV_F32 or ICV_BF16, per block:
+ *   scale = max|x| / 448, at least 2^-126; 1 for a block of zeros;  code = x / scale rounded to e4m3 (to nearest, ties
+ *   to even; both divisions in float).  NaN elements become the code NaN and do not enter the maximum; with an infinite one the scale is
+ *   infinite, infinite elements become NaN and the others zeros.
+ * block_rows = 1 is for activations (a row's scales do not depend on the other rows), 128 for filters.
+ *   input : [rows] rows of in_row_stride elements, only their element's alignment
+ *   codes : [rows] rows of code_row_stride bytes, 16-byte aligned; all ceil(depth/128)*128 bytes of a row are written
+ *   scales: [ceil(depth/128)][ceil(rows/block_rows)] floats
+ */
+typedef struct icv_quantize_params {
+    int32_t rows, depth;
+    int32_t block_rows;             /* 1 or 128 */
+    int32_t dtype;                  /* ICV_F32 or ICV_BF16 */
+    int32_t in_row_stride;          /* 0 means depth */
+    int32_t code_row_stride;        /* 0 means ceil(depth/128)*128; a multiple of 16, no less than that */
+} icv_quantize_params;
+ICV_API int icv_quantize_fp8(const icv_quantize_params* p, const void* input, void* codes, float* scales, void* stream);
+
+/*
+ * out[m][n] = bias[n] + sum over k of a[m][k] * b[n][k]: the pointwise convolution with rows of pixels a and the
+ * filter b ([K][C], section 3.2's plain GEMM), both in the form above, a with block_rows 1, b with 128.  A block's sum
+ * of 128 products is multiplied by the block's two scales and added to a float sum.  For a float output all of it is
+ * float arithmetic; for a bfloat16 output a block's products are summed by the e4m3 instruction, which cuts each to 13
+ * bits below the largest of its 8 neighbours (about 1.5e-5 of the result).  rows = 0: nothing to do, ICV_OK.
+ *   a, b  : 16-byte aligned; a_scales [ceil(depth/128)][rows], b_scales [ceil(depth/128)][ceil(cols/128)]
+ *   bias  : cols floats or NULL
+ *   out   : [rows] rows of out_row_stride elements: float (ICV_OUT_ACC) or bfloat16 (ICV_OUT_BF16)
+ */
+typedef struct icv_matmul_params {
+    int32_t rows, cols, depth;
+    int32_t a_row_stride, b_row_stride;   /* bytes; 0 means ceil(depth/128)*128 */
+    int32_t out_row_stride;               /* elements; 0 means cols */
+    int32_t out_type;                     /* ICV_OUT_ACC or ICV_OUT_BF16 */
+} icv_matmul_params;
+ICV_API int icv_matmul_fp8(const icv_matmul_params* p, const void* a, const float* a_scales, const void* b,
+                           const float* b_scales, const float* bias, void* out, void* stream);
 
 /*
  * Measurement aid: the rate, in multiply-add operations times two per second, at which the current device runs a

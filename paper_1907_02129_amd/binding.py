@@ -33,6 +33,7 @@ EXPORTS = (
     "icv_tile_span_bound", "icv_init_zero_row", "icv_pack_filter",
     "icv_setup_indirection", "icv_conv2d_nhwc", "icv_conv2d_nhwc_fused", "icv_im2col", "icv_gemm_nhwc", "icv_conv2d_nhwc_im2col",
     "icv_static_workspace_bytes", "icv_conv2d_nhwc_im2col_static",
+    "icv_causal_conv1d", "icv_selective_scan_workspace_bytes", "icv_selective_scan", "icv_quantize_fp8", "icv_matmul_fp8",
     "icv_plan_name", "icv_status_string", "icv_last_hip_error", "icv_measure_mfma_peak",
 )
 
@@ -61,6 +62,36 @@ class icv_indirection_layout(ctypes.Structure):
     _fields_ = [("tile_rows", ctypes.c_int32), ("entry_bytes", ctypes.c_int32), ("zero_code", ctypes.c_int32),
                 ("record_bytes", ctypes.c_int32), ("tiles", ctypes.c_int64), ("entries_at", ctypes.c_int64),
                 ("records_at", ctypes.c_int64), ("int32_entries_at", ctypes.c_int64)]
+
+
+class icv_sequences(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int32), ("tokens", ctypes.c_int32), ("start", ctypes.c_void_p),
+                ("length", ctypes.c_void_p), ("from_", ctypes.c_void_p), ("to", ctypes.c_void_p)]
+
+
+class icv_causal_conv_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "channels", "taps", "in_row_stride", "out_row_stride", "dtype", "silu", "state_slots")] + [
+        ("state_slot_stride", ctypes.c_int64)]
+
+
+class icv_scan_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "channels", "states", "groups", "x_row_stride", "dt_row_stride", "b_row_stride", "c_row_stride", "z_row_stride",
+        "out_row_stride", "dtype", "softplus", "state_slots")] + [("state_slot_stride", ctypes.c_int64)]
+
+
+class icv_scan_tensors(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "dt", "A", "B", "C", "D", "z", "dt_bias", "state", "out")]
+
+
+class icv_quantize_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "depth", "block_rows", "dtype", "in_row_stride", "code_row_stride")]
+
+
+class icv_matmul_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "rows", "cols", "depth", "a_row_stride", "b_row_stride", "out_row_stride", "out_type")]
 
 
 ICV_OUT_ACC, ICV_OUT_BF16, ICV_OUT_U8 = 0, 1, 2
@@ -100,6 +131,14 @@ def load_library(path: str | None = None):
         "icv_conv2d_nhwc_im2col": (ctypes.c_int, [P, vp, vp, vp, vp, vp]),
         "icv_static_workspace_bytes": (ctypes.c_size_t, []),
         "icv_conv2d_nhwc_im2col_static": (ctypes.c_int, [P, vp, vp, vp, vp]),
+        "icv_causal_conv1d": (ctypes.c_int, [ctypes.POINTER(icv_causal_conv_params), ctypes.POINTER(icv_sequences),
+                                             vp, vp, vp, vp, vp, vp]),
+        "icv_selective_scan_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(icv_scan_params),
+                                                                 ctypes.POINTER(icv_sequences)]),
+        "icv_selective_scan": (ctypes.c_int, [ctypes.POINTER(icv_scan_params), ctypes.POINTER(icv_sequences),
+                                              ctypes.POINTER(icv_scan_tensors), vp, vp]),
+        "icv_quantize_fp8": (ctypes.c_int, [ctypes.POINTER(icv_quantize_params), vp, vp, vp, vp]),
+        "icv_matmul_fp8": (ctypes.c_int, [ctypes.POINTER(icv_matmul_params), vp, vp, vp, vp, vp, vp, vp]),
         "icv_plan_name": (ctypes.c_char_p, [P]),
         "icv_measure_mfma_peak": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_double),
                                                  ctypes.c_void_p]),
@@ -256,6 +295,162 @@ def static_workspace_bytes() -> int:
 def conv2d_nhwc_im2col_static(p, input, packed_filter, output, stream=None):
     _check(load_library().icv_conv2d_nhwc_im2col_static(ctypes.byref(p), _ptr(input), _ptr(packed_filter), _ptr(output),
                                                         _stream(stream)), "icv_conv2d_nhwc_im2col_static")
+
+
+# ---------------------------------------------------------------- operators on sequences and in 8-bit floating point
+# These take views (a slice of a wider matrix is the usual input), so the tensors are checked against the problem's
+# description here: the library sees addresses only.  Lists of (tensor, rows, columns, row stride, type).
+_TORCH = {ICV_F32: torch.float32, ICV_BF16: torch.bfloat16}
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _matrix(name, t, rows, cols, stride, dtype):
+    """Address of a [rows][cols] matrix whose rows lie `stride` elements apart."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: icv takes device tensors")
+    if (t.dtype not in dtype) if isinstance(dtype, tuple) else (t.dtype is not dtype):
+        raise ValueError(f"{name}: type {t.dtype}, expected {dtype}")
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] < rows or shape[1] < cols:
+        raise ValueError(f"{name}: shape {tuple(shape)}, at least {(rows, cols)} expected")
+    if (cols > 1 and strides[1] != 1) or (rows > 1 and strides[0] != stride):
+        raise ValueError(f"{name}: strides {tuple(strides)}, {(stride, 1)} expected")
+    return t.data_ptr()
+
+
+def _vector(name, t, n, dtype, optional=True):
+    """Address of a contiguous tensor of at least n elements; None for none."""
+    if t is None and optional:
+        return None
+    if not t.is_cuda or t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous device tensor of {dtype} with at least {n} elements expected")
+    return t.data_ptr()
+
+
+def _slots(name, t, slots, per_slot, slot_stride, dtype):
+    """Address of at least `slots` state slots of per_slot elements, each contiguous, slot_stride apart; None for none."""
+    if t is None or per_slot == 0:
+        return None
+    shape = t.shape
+    if not t.is_cuda or t.dtype is not dtype or len(shape) < 2 or shape[0] < slots or t.numel() != shape[0] * per_slot or (
+            slots > 1 and t.stride(0) != slot_stride) or not (t.is_contiguous() or (slots > 0 and t[0].is_contiguous())):
+        raise ValueError(f"{name}: {slots} device slots of {per_slot} elements of {dtype}, {slot_stride} apart, expected")
+    return t.data_ptr()
+
+
+def _stream_of(tensors, stream):
+    """The raw stream to launch on, and the device to be current meanwhile (None: it is): the tensors' own, which must
+    be one."""
+    device = tensors[0].device
+    if device.type != "cuda":
+        raise ValueError("icv takes device tensors")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("icv takes tensors of one device")
+    if stream is not None and stream.device != device:
+        raise ValueError("the stream is another device's")
+    raw = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
+    return raw, None if device.index == torch.cuda.current_device() else device
+
+
+def _call(where, device, fn, *args):
+    if device is None:
+        _check(fn(*args), where)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args), where)
+
+
+def make_sequences(count, tokens, start=None, length=None, from_slot=None, to_slot=None) -> icv_sequences:
+    """icv_sequences; the arrays are int32 device tensors, kept alive by the result.  `start` has count + 1 entries, the
+    others count; what they hold is read when the kernels run."""
+    s = icv_sequences(count, tokens, _vector("start", start, count + 1, torch.int32), _vector("length", length, count, torch.int32),
+                      _vector("from_slot", from_slot, count, torch.int32), _vector("to_slot", to_slot, count, torch.int32))
+    s.arrays = [t for t in (start, length, from_slot, to_slot) if t is not None]
+    return s
+
+
+def make_causal_conv_params(channels, taps, dtype="bf16", silu=True, in_row_stride=0, out_row_stride=0, state_slots=0,
+                            state_slot_stride=0) -> icv_causal_conv_params:
+    return icv_causal_conv_params(channels, taps, in_row_stride, out_row_stride, DTYPES[dtype], int(silu), state_slots,
+                                  state_slot_stride)
+
+
+def causal_conv1d(p, seq, input, filter, bias, state, output, stream=None):
+    """Short causal convolution (icv_causal_conv1d): input and output [tokens, channels], filter [channels, taps], bias
+    [channels] or None, state [slots, taps - 1, channels] (read and written) or None."""
+    raw, device = _stream_of([input, filter, bias, state, output, *getattr(seq, "arrays", ())], stream)
+    t, D, W = _TORCH.get(p.dtype), p.channels, p.taps
+    _call("icv_causal_conv1d", device, load_library().icv_causal_conv1d, p, seq,
+          _matrix("input", input, seq.tokens, D, p.in_row_stride or D, t), _vector("filter", filter, D * W, t, False),
+          _vector("bias", bias, D, torch.float32),
+          _slots("state", state, p.state_slots, (W - 1) * D, p.state_slot_stride or (W - 1) * D, t),
+          _matrix("output", output, seq.tokens, D, p.out_row_stride or D, t), raw)
+
+
+def make_scan_params(channels, states, dtype="bf16", groups=1, softplus=True, x_row_stride=0, dt_row_stride=0, b_row_stride=0,
+                     c_row_stride=0, z_row_stride=0, out_row_stride=0, state_slots=0, state_slot_stride=0) -> icv_scan_params:
+    return icv_scan_params(channels, states, groups, x_row_stride, dt_row_stride, b_row_stride, c_row_stride, z_row_stride,
+                           out_row_stride, DTYPES[dtype], int(softplus), state_slots, state_slot_stride)
+
+
+def selective_scan_workspace_bytes(p, seq) -> int:
+    return load_library().icv_selective_scan_workspace_bytes(p, seq)
+
+
+def selective_scan(p, seq, x, dt, A, B, C, D, z, dt_bias, state, output, workspace=None, stream=None):
+    """Selective scan (icv_selective_scan): x, dt, z, output [tokens, channels], B, C [tokens, groups * states], A [channels,
+    states], D, dt_bias [channels]; D, z, dt_bias and state [slots, channels, states] (read and written) may be None.  `workspace`: a device tensor of
+    selective_scan_workspace_bytes() bytes at least, which may be None where that is 0."""
+    raw, device = _stream_of([x, dt, A, B, C, D, z, dt_bias, state, output, workspace, *getattr(seq, "arrays", ())], stream)
+    t, n, ch, bc, f32 = _TORCH.get(p.dtype), seq.tokens, p.channels, p.groups * p.states, torch.float32
+    lib = load_library()
+    need = lib.icv_selective_scan_workspace_bytes(p, seq)
+    if need and (workspace is None or not workspace.is_contiguous() or workspace.numel() * workspace.element_size() < need):
+        raise ValueError(f"workspace: a contiguous device tensor of at least {need} bytes expected")
+    tensors = icv_scan_tensors(
+        _matrix("x", x, n, ch, p.x_row_stride or ch, t), _matrix("dt", dt, n, ch, p.dt_row_stride or ch, t),
+        _vector("A", A, ch * p.states, f32, False), _matrix("B", B, n, bc, p.b_row_stride or bc, t),
+        _matrix("C", C, n, bc, p.c_row_stride or bc, t), _vector("D", D, ch, f32),
+        None if z is None else _matrix("z", z, n, ch, p.z_row_stride or ch, t), _vector("dt_bias", dt_bias, ch, f32),
+        _slots("state", state, p.state_slots, ch * p.states, p.state_slot_stride or ch * p.states, f32),
+        _matrix("output", output, n, ch, p.out_row_stride or ch, t))
+    _call("icv_selective_scan", device, lib.icv_selective_scan, p, seq, tensors,
+          workspace.data_ptr() if need else None, raw)
+
+
+def make_quantize_params(rows, depth, dtype="bf16", block_rows=1, in_row_stride=0, code_row_stride=0) -> icv_quantize_params:
+    return icv_quantize_params(rows, depth, block_rows, DTYPES[dtype], in_row_stride, code_row_stride)
+
+
+def quantize_fp8(p, input, codes, scales, stream=None):
+    """Quantisation into e4m3 (icv_quantize_fp8): input [rows, depth], codes [rows, depth up to a multiple of 128] of
+    float8_e4m3fn or uint8, scales [blocks of 128 columns, blocks of rows]."""
+    raw, device = _stream_of([input, codes, scales], stream)
+    kb, br = -(-p.depth // 128), max(1, p.block_rows)
+    _call("icv_quantize_fp8", device, load_library().icv_quantize_fp8, p,
+          _matrix("input", input, p.rows, p.depth, p.in_row_stride or p.depth, _TORCH.get(p.dtype)),
+          _matrix("codes", codes, p.rows, 128 * kb, p.code_row_stride or 128 * kb, _CODES),
+          _vector("scales", scales, kb * -(-p.rows // br), torch.float32, False), raw)
+
+
+def make_matmul_params(rows, cols, depth, out="bf16", a_row_stride=0, b_row_stride=0, out_row_stride=0) -> icv_matmul_params:
+    return icv_matmul_params(rows, cols, depth, a_row_stride, b_row_stride, out_row_stride,
+                             {"f32": ICV_OUT_ACC, "bf16": ICV_OUT_BF16}[out])
+
+
+def matmul_fp8(p, a, a_scales, b, b_scales, bias, output, stream=None):
+    """output = a @ b.T + bias with e4m3 operands (icv_matmul_fp8): a [rows, depth up to a multiple of 128] and b [cols, the
+    same] of float8_e4m3fn or uint8 with their scales from quantize_fp8 (block_rows 1 and 128), bias [cols] or None."""
+    raw, device = _stream_of([a, a_scales, b, b_scales, bias, output], stream)
+    kb, f32 = -(-p.depth // 128), torch.float32
+    _call("icv_matmul_fp8", device, load_library().icv_matmul_fp8, p,
+          _matrix("a", a, p.rows, 128 * kb, p.a_row_stride or 128 * kb, _CODES),
+          _vector("a_scales", a_scales, kb * p.rows, f32, False),
+          _matrix("b", b, p.cols, 128 * kb, p.b_row_stride or 128 * kb, _CODES),
+          _vector("b_scales", b_scales, kb * -(-p.cols // 128), f32, False), _vector("bias", bias, p.cols, f32),
+          _matrix("output", output, p.rows, p.cols, p.out_row_stride or p.cols,
+                  f32 if p.out_type == ICV_OUT_ACC else torch.bfloat16), raw)
 
 
 # ---------------------------------------------------------------- convenience: buffers for one problem

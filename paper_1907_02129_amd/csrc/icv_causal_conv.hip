@@ -1,0 +1,190 @@
+// Short causal convolution along sequences (icv_causal_conv1d).
+//
+// Memory bound: 2 * taps operations per element read and written.  A thread owns VEC neighbouring channels (16 bytes of a
+// row) over a run of consecutive rows, keeps the last taps - 1 rows in registers as floats, and so reads every row
+// once, plus taps - 1 rows in front of its run.  Runs are counted over all rows of the call, whatever sequences they
+// belong to, so that ragged batches load the chip evenly; a thread walks the sequences that its run meets.
+//
+// The state may be read and written in the same slot, so one thread does both: the run that holds a sequence's first
+// row computes the sequence's first taps - 1 rows (all rows that the old state reaches), also where they pass the run's
+// end, and writes the new state; the runs behind it leave those rows out.
+#include "icv_sequence.h"
+
+namespace icv {
+
+struct ConvArgs {
+    const void* in;
+    const void* filt;
+    const float* bias;
+    void* state;
+    void* out;
+    int32_t channels, vecs, run, silu;
+    int64_t in_stride, out_stride, slot_stride;
+    SeqArgs seq;
+};
+
+template <typename T, int W, int VEC>
+__global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
+{
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int32_t runs = (a.seq.tokens + a.run - 1) / a.run;
+    const int64_t r = id / a.vecs;
+    if (r >= runs) return;
+    const int32_t c0 = (int32_t)(id - r * a.vecs) * VEC;
+    const int32_t nv = a.channels - c0 < VEC ? a.channels - c0 : VEC;
+    const T* in = (const T*)a.in + c0;
+    T* out = (T*)a.out + c0;
+    T* state = (T*)a.state + c0;
+    const int32_t r0 = (int32_t)r * a.run, r1 = a.seq.tokens - r0 < a.run ? a.seq.tokens : r0 + a.run;
+
+    float w[W][VEC], bias[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; j++) {
+        const int32_t c = c0 + (j < nv ? j : 0);
+        bias[j] = a.bias ? a.bias[c] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < W; k++) w[k][j] = (float)((const T*)a.filt)[(int64_t)c * W + k];
+    }
+
+    // the last sequence that begins at or before the run's first row, else the first one
+    int32_t i = 0;
+    if (a.seq.start) {
+        int32_t lo = 0, hi = a.seq.count;              // begin(lo) <= r0 < begin(hi), if any begins there
+        while (hi - lo > 1) {
+            const int32_t mid = (lo + hi) >> 1;
+            if (seq_begin(a.seq, mid) <= r0) lo = mid; else hi = mid;
+        }
+        i = lo;
+    } else {
+        i = r0 / a.seq.each;
+    }
+    for (; i < a.seq.count; i++) {
+        const int32_t b = seq_begin(a.seq, i);
+        if (b >= r1) break;
+        const int32_t e = seq_end(a.seq, i, b);
+        if (e == b) continue;
+        const bool owner = b >= r0;                     // the run that holds the sequence's first row
+        const int32_t own_end = e - b < W - 1 ? e : b + W - 1;
+        int32_t lo = owner ? b : (r0 > own_end ? r0 : own_end);
+        int32_t hi = e < r1 ? e : r1;
+        if (owner && hi < own_end) hi = own_end;
+        if (lo >= hi) continue;
+
+        float win[W > 1 ? W - 1 : 1][VEC], old[W > 1 ? W - 1 : 1][VEC];
+        if (owner) {
+            const int32_t slot = a.state ? seq_slot(a.seq, a.seq.from, i) : -1;
+#pragma unroll
+            for (int k = 0; k < W - 1; k++) {
+#pragma unroll
+                for (int j = 0; j < VEC; j++) old[k][j] = 0.0f;
+                if (slot >= 0) load_row<VEC>(state + slot * a.slot_stride + (int64_t)k * a.channels, nv, old[k]);
+#pragma unroll
+                for (int j = 0; j < VEC; j++) win[k][j] = old[k][j];
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < W - 1; k++) load_row<VEC>(in + (int64_t)(lo - (W - 1) + k) * a.in_stride, nv, win[k]);
+        }
+        for (int32_t t = lo; t < hi; t++) {
+            float x[VEC], y[VEC];
+            load_row<VEC>(in + (int64_t)t * a.in_stride, nv, x);
+#pragma unroll
+            for (int j = 0; j < VEC; j++) {
+                float s = bias[j];
+#pragma unroll
+                for (int k = 0; k < W - 1; k++) s = fmaf(w[k][j], win[k][j], s);
+                s = fmaf(w[W - 1][j], x[j], s);
+                y[j] = a.silu ? silu(s) : s;
+            }
+            store_row<VEC>(out + (int64_t)t * a.out_stride, nv, y);
+            if constexpr (W > 1) {
+#pragma unroll
+                for (int k = 0; k + 1 < W - 1; k++)
+#pragma unroll
+                    for (int j = 0; j < VEC; j++) win[k][j] = win[k + 1][j];
+#pragma unroll
+                for (int j = 0; j < VEC; j++) win[W - 2][j] = x[j];
+            }
+        }
+        const int32_t slot = owner && a.state ? seq_slot(a.seq, a.seq.to, i) : -1;
+        if (W > 1 && slot >= 0) {
+#pragma unroll
+            for (int k = 0; k < W - 1; k++) {
+                const int32_t at = e - b - (W - 1) + k;  // the sequence's row that becomes state row k; below 0 an old one
+                float v[VEC];
+                if (at >= 0) {
+                    load_row<VEC>(in + (int64_t)(b + at) * a.in_stride, nv, v);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < VEC; j++) v[j] = 0.0f;
+#pragma unroll
+                    for (int q = 1; q < W - 1; q++)
+                        if (q == W - 1 + at)
+#pragma unroll
+                            for (int j = 0; j < VEC; j++) v[j] = old[q][j];
+                }
+                store_row<VEC>(state + slot * a.slot_stride + (int64_t)k * a.channels, nv, v);
+            }
+        }
+    }
+}
+
+template <typename T, int W>
+static int launch(ConvArgs a, hipStream_t s)
+{
+    constexpr int VEC = 16 / sizeof(T);
+    a.vecs = (a.channels + VEC - 1) / VEC;
+    a.run = a.seq.start || a.seq.each > 1 ? 16 : 1;
+    const int64_t threads = (int64_t)a.vecs * ((a.seq.tokens + a.run - 1) / a.run);
+    const int64_t blocks = (threads + 255) / 256;
+    if (blocks > INT32_MAX) return ICV_ERR_INVALID_ARG;
+    k_causal_conv<T, W, VEC><<<(uint32_t)blocks, 256, 0, s>>>(a);
+    ICV_HIP_CHECK(hipGetLastError());
+    return ICV_OK;
+}
+
+template <typename T>
+static int launch_taps(const ConvArgs& a, int taps, hipStream_t s)
+{
+    switch (taps) {
+        case 1: return launch<T, 1>(a, s);
+        case 2: return launch<T, 2>(a, s);
+        case 3: return launch<T, 3>(a, s);
+        case 4: return launch<T, 4>(a, s);
+        case 5: return launch<T, 5>(a, s);
+        case 6: return launch<T, 6>(a, s);
+        case 7: return launch<T, 7>(a, s);
+        default: return launch<T, 8>(a, s);
+    }
+}
+
+}  // namespace icv
+
+extern "C" int icv_causal_conv1d(const icv_causal_conv_params* p, const icv_sequences* seq, const void* input,
+                                 const void* filter, const float* bias, void* state, void* output, void* stream)
+{
+    using namespace icv;
+    if (!p || p->channels < 1 || p->taps < 1 || p->taps > 8 || (p->silu != 0 && p->silu != 1)) return ICV_ERR_INVALID_ARG;
+    if (p->dtype == ICV_U8I8) return ICV_ERR_UNSUPPORTED;
+    if (p->dtype != ICV_F32 && p->dtype != ICV_BF16) return ICV_ERR_INVALID_ARG;
+    if ((p->in_row_stride && p->in_row_stride < p->channels) || (p->out_row_stride && p->out_row_stride < p->channels))
+        return ICV_ERR_INVALID_ARG;
+    const int64_t slot = (int64_t)(p->taps - 1) * p->channels;
+    if (p->state_slots < 0 || (p->state_slot_stride && p->state_slot_stride < slot)) return ICV_ERR_INVALID_ARG;
+    ConvArgs a;
+    const int st = make_seq_args(seq, p->state_slots, &a.seq);
+    if (st != ICV_OK) return st;
+    if (seq->count == 0 || seq->tokens == 0) return ICV_OK;
+    const uintptr_t size = p->dtype == ICV_F32 ? 4 : 2;
+    if (!input || !filter || !output || input == output) return ICV_ERR_INVALID_ARG;
+    if (misaligned(input, size) || misaligned(filter, size) || misaligned(output, size) || misaligned(state, size) ||
+        misaligned(bias, 4))
+        return ICV_ERR_INVALID_ARG;
+    a.in = input; a.filt = filter; a.bias = bias; a.state = state; a.out = output;
+    a.channels = p->channels; a.silu = p->silu;
+    a.in_stride = p->in_row_stride ? p->in_row_stride : p->channels;
+    a.out_stride = p->out_row_stride ? p->out_row_stride : p->channels;
+    a.slot_stride = p->state_slot_stride ? p->state_slot_stride : slot;
+    hipStream_t s = (hipStream_t)stream;
+    return p->dtype == ICV_F32 ? launch_taps<float>(a, p->taps, s) : launch_taps<__bf16>(a, p->taps, s);
+}

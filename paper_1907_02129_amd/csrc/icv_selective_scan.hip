@@ -1,0 +1,468 @@
+// Selective state space scan (icv_selective_scan).
+//
+// Per row, channel and state: one exponential (the decay), two products and two multiply-adds.  Vector-ALU bound: about
+// 24 issue cycles for 64 of them (8 for the exponential, 4 for each of the others), against 2 to 8 bytes of memory
+// per row and channel.
+//
+// A lane keeps 4 states of a channel in registers, S lanes (1..16) a channel: the rows' delta and delta * x are then read
+// from LDS once for 4 states, and a channel's states take few enough registers for several workgroups on a compute
+// unit, whose wavefronts hide each other's latencies.  A workgroup of 256 lanes owns 256 / S channels of one group
+// (they share B and C) and walks a sequence in tiles of TT rows: the next tile's inputs are on their way from memory
+// while this one's rows are stepped through from LDS; softplus and the products with x are computed once per row and
+// channel when a tile is staged, and D * x and the gate once when it is stored.  The sums over a channel's lanes are
+// taken for four rows at a time, by exchanges inside quads that leave each lane with one row's sum.
+#include "icv_sequence.h"
+
+namespace icv {
+
+struct ScanArgs {
+    const void *x, *dt, *B, *C, *z;
+    const float *A, *D, *dtb;
+    float* state;
+    void* out;
+    int64_t xs, dts, bs, cs, zs, os, slot_stride;
+    int32_t channels, states, per_group, group_tiles, softplus;
+    int32_t chunk, units;     // rows per piece of a sequence (0: sequences are not cut), pieces there is room for
+    float *ws_state, *ws_sum; // of every piece: [channels][states] and [channels]
+    SeqArgs seq;
+};
+
+enum { SCAN_WHOLE = 0, SCAN_PIECE_STATE = 1, SCAN_PIECE_OUT = 2 };
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+// log(1 + exp(v)).  With e = exp(v) and u = 1 + e rounded, log(1 + e) = log(u) + log(1 + (e - (u - 1)) / u), the second
+// term being a rounding error small enough for its first order: exact to a few ulp for every v, tiny e included.
+__device__ inline float softplus(float v)
+{
+    const float e = __builtin_amdgcn_exp2f(v * kLog2e), u = 1.0f + e;
+    const float s = fmaf(__builtin_amdgcn_logf(u), kLn2, (e - (u - 1.0f)) * __builtin_amdgcn_rcpf(u));
+    return v > 20.0f ? v : s;         // exp(-20) is below half an ulp of 20
+}
+
+template <int N, typename T>
+__device__ inline void load_raw(const T* p, int n, T (&r)[N])
+{
+    if (n >= N) {
+        __builtin_memcpy(r, p, sizeof(r));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; j++) r[j] = j < n ? p[j] : (T)0.0f;
+    }
+}
+
+// lane -> its place among the S lanes of a channel, and the channel among the wavefront's.  The four lowest states of a
+// channel sit in one quad; with 8 lanes the second quad is 8 lanes away, with 16 all of a row of 16 is one channel's,
+// so that the sums over quads are rotations within a row.
+template <int S>
+__device__ inline void lane_place(int lane, int* s, int* ch)
+{
+    if constexpr (S == 8) { *s = (lane & 3) | ((lane >> 1) & 4); *ch = ((lane >> 4) << 1) | ((lane >> 2) & 1); }
+    else { *s = lane & (S - 1); *ch = lane / S; }
+}
+
+template <int CTRL>
+__device__ inline float dpp(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kRotate4 = 0x124, kRotate8 = 0x128;
+
+// Sums over the S lanes of a channel of four rows' partial sums.  S >= 4: lane s returns row s & 3's; S = 2: lane s returns
+// rows s and s + 2; S = 1: all four.
+template <int S>
+__device__ inline void reduce_rows(const float (&p)[4], int s, float (&y)[4])
+{
+    if constexpr (S == 1) {
+#pragma unroll
+        for (int u = 0; u < 4; u++) y[u] = p[u];
+        return;
+    }
+    const bool odd = s & 1, high = s & 2;
+    const float q0 = (odd ? p[1] : p[0]) + dpp<kXor1>(odd ? p[0] : p[1]);
+    const float q1 = (odd ? p[3] : p[2]) + dpp<kXor1>(odd ? p[2] : p[3]);
+    y[0] = q0; y[1] = q1;
+    if constexpr (S >= 4) {
+        float r = (high ? q1 : q0) + dpp<kXor2>(high ? q0 : q1);
+        if constexpr (S == 16) r += dpp<kRotate4>(r);
+        if constexpr (S >= 8) r += dpp<kRotate8>(r);
+        y[0] = r;
+    }
+}
+
+// The states a lane holds: n..n+3 of channel d, `nv` of them real.
+__device__ inline void load_states(const float* p, int nv, float (&h)[4])
+{
+    load_row<4>(p, nv, h);
+}
+
+template <typename T, int S, bool PAD, int MODE>
+__global__ __launch_bounds__(256) void k_scan(ScanArgs a)
+{
+    constexpr int CW = 256 / S, TT = 8 * S < 64 ? 8 * S : 64, PPT = TT * CW / 256, VPR = CW / PPT;
+    constexpr int BCV = (TT * S + 255) / 256;      // vectors of 4 states of B (and C) a thread stages
+    __shared__ float2 dtx[TT][CW];                  // delta and delta * x; the row's output takes delta's place
+    __shared__ float4 sB[TT][S], sC[MODE == SCAN_PIECE_STATE ? 1 : TT][S];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int32_t tiles = a.group_tiles * (a.channels / a.per_group);
+    const int32_t tile = (int32_t)(blockIdx.x % tiles);
+    int32_t unit = (int32_t)(blockIdx.x / tiles), piece = 0, pieces = 1, i = unit;
+    int32_t begin, end;
+    if (MODE == SCAN_WHOLE) {
+        begin = seq_begin(a.seq, i);
+        end = seq_end(a.seq, i, begin);
+        if (begin == end) return;
+    } else {
+        // the sequence that piece `unit` belongs to, counting every sequence's pieces
+        int32_t left = unit;
+        for (i = 0;; i++) {
+            if (i == a.seq.count) return;
+            begin = seq_begin(a.seq, i);
+            end = seq_end(a.seq, i, begin);
+            pieces = (end - begin + a.chunk - 1) / a.chunk;
+            if (left < pieces) break;
+            left -= pieces;
+        }
+        piece = left;
+        if (MODE == SCAN_PIECE_STATE && piece == pieces - 1) return;
+    }
+    const int32_t first_unit = unit - piece;
+    if (MODE != SCAN_WHOLE && first_unit + pieces > a.units) return;      // sequences that overlap: more pieces than there is room for
+    const int32_t row0 = begin + piece * a.chunk;
+    const int32_t row1 = MODE == SCAN_WHOLE || piece == pieces - 1 ? end : row0 + a.chunk;
+
+    const int32_t group = tile / a.group_tiles, tile_c = (tile - group * a.group_tiles) * CW;
+    const int32_t c0 = group * a.per_group + tile_c;                  // the tile's first channel
+    const int32_t cn = a.per_group - tile_c < CW ? a.per_group - tile_c : CW;
+
+    int s, wch;
+    lane_place<S>(lane, &s, &wch);
+    const int ch = (tid >> 6) * (64 / S) + wch;
+    const int32_t d = c0 + (ch < cn ? ch : 0);
+    const int nv = a.states - 4 * s < 0 ? 0 : (a.states - 4 * s < 4 ? a.states - 4 * s : 4);
+
+    float A[4], h[4];
+    load_states(a.A + (int64_t)d * a.states + 4 * s, nv, A);
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        A[j] *= kLog2e;
+        A[j] = A[j] < -3.0e38f ? -3.0e38f : A[j];     // rows past the end step by 0 * A, which has to be 0
+    }
+
+    const int64_t state_at = (int64_t)d * a.states + 4 * s;
+    const int64_t plane = (int64_t)a.channels * a.states;
+#pragma unroll
+    for (int j = 0; j < 4; j++) h[j] = 0.0f;
+    if (piece == 0 && !(MODE == SCAN_PIECE_OUT && pieces > 1)) {
+        const int32_t slot = a.state ? seq_slot(a.seq, a.seq.from, i) : -1;
+        if (slot >= 0) load_states(a.state + slot * a.slot_stride + state_at, nv, h);
+        // the slot may be written while the pieces' outputs are computed: those read the copy in the last piece's place
+        if (MODE == SCAN_PIECE_STATE && ch < cn) store_row<4>(a.ws_state + (first_unit + pieces - 1) * plane + state_at, nv, h);
+    } else if (MODE == SCAN_PIECE_OUT) {
+        load_states(a.ws_state + (piece == 0 ? first_unit + pieces - 1 : first_unit) * plane + state_at, nv, h);
+        for (int32_t q = 1; q < piece; q++) {
+            const float sum = a.ws_sum[(int64_t)(first_unit + q) * a.channels + d];
+            float w[4];
+            load_states(a.ws_state + (first_unit + q) * plane + state_at, nv, w);
+#pragma unroll
+            for (int j = 0; j < 4; j++) h[j] = fmaf(__builtin_amdgcn_exp2f(sum * A[j]), h[j], w[j]);
+        }
+    }
+
+    // staging: thread -> row and PPT channels of the tile, and vectors of B and C
+    const int vrow = tid / VPR, vch = (tid % VPR) * PPT;
+    const int vn = cn - vch < 0 ? 0 : (cn - vch < PPT ? cn - vch : PPT);
+    float dtb[PPT], Dx[PPT];
+#pragma unroll
+    for (int j = 0; j < PPT; j++) {
+        dtb[j] = a.dtb && j < vn ? a.dtb[c0 + vch + j] : 0.0f;
+        Dx[j] = a.D && j < vn ? a.D[c0 + vch + j] : 0.0f;
+    }
+    const T* xp = (const T*)a.x + c0 + vch;
+    const T* dtp = (const T*)a.dt + c0 + vch;
+    const T* zp = (const T*)a.z + c0 + vch;
+    T* op = (T*)a.out + c0 + vch;
+    T nx[PPT], nd[PPT], nz[PPT], nB[BCV][4], nC[BCV][4];
+    auto fetch = [&](int32_t r) {
+        const int n = r + vrow < row1 ? vn : 0;
+        const int64_t t = n ? r + vrow : row0;
+        load_raw<PPT>(xp + t * a.xs, n, nx);
+        load_raw<PPT>(dtp + t * a.dts, n, nd);
+        if (MODE != SCAN_PIECE_STATE && a.z) load_raw<PPT>(zp + t * a.zs, n, nz);
+#pragma unroll
+        for (int q = 0; q < BCV; q++) {
+            const int v = tid + 256 * q, row = v / S, n4 = 4 * (v % S);
+            if (TT * S % 256 != 0 && row >= TT) continue;
+            int m = a.states - n4 < 0 ? 0 : (a.states - n4 < 4 ? a.states - n4 : 4);
+            if (r + row >= row1) m = 0;
+            const int64_t tb = m ? r + row : row0;
+            load_raw<4>((const T*)a.B + tb * a.bs + (int64_t)group * a.states + (m ? n4 : 0), m, nB[q]);
+            if (MODE != SCAN_PIECE_STATE)
+                load_raw<4>((const T*)a.C + tb * a.cs + (int64_t)group * a.states + (m ? n4 : 0), m, nC[q]);
+        }
+    };
+
+    float total = 0.0f;                       // sum of delta over the piece
+    fetch(row0);
+    for (int32_t r = row0; r < row1; r += TT) {
+        const int n = r + vrow < row1 ? vn : 0;
+        T cx[PPT], cz[PPT];
+#pragma unroll
+        for (int j = 0; j < PPT; j++) {
+            cx[j] = nx[j]; cz[j] = nz[j];
+            float v = (float)nd[j] + dtb[j];
+            if (a.softplus) v = softplus(v);
+            if (j >= n) v = 0.0f;             // rows past the end and channels past the tile: decay 1, nothing added
+            dtx[vrow][vch + j] = make_float2(v, j < n ? v * (float)nx[j] : 0.0f);
+        }
+#pragma unroll
+        for (int q = 0; q < BCV; q++) {
+            const int v = tid + 256 * q, row = v / S, sv = v % S;
+            if (TT * S % 256 != 0 && row >= TT) continue;
+            sB[row][sv] = make_float4((float)nB[q][0], (float)nB[q][1], (float)nB[q][2], (float)nB[q][3]);
+            if (MODE != SCAN_PIECE_STATE)
+                sC[row][sv] = make_float4((float)nC[q][0], (float)nC[q][1], (float)nC[q][2], (float)nC[q][3]);
+        }
+        __syncthreads();
+        if (r + TT < row1) fetch(r + TT);
+
+        const int rows = row1 - r < TT ? row1 - r : TT;
+        for (int t = 0; t < rows; t += 4) {
+            float p[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const float2 v = dtx[t + u][ch];
+                const float4 b = sB[t + u][s];
+                const float bb[4] = {b.x, b.y, b.z, b.w};
+                p[u] = 0.0f;
+                if (MODE == SCAN_PIECE_STATE) total += v.x;
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    h[j] = fmaf(__builtin_amdgcn_exp2f(v.x * A[j]), h[j], v.y * bb[j]);
+                    if (PAD) h[j] = j < nv ? h[j] : 0.0f;    // an infinite input must not reach a state that is not there
+                }
+                if (MODE != SCAN_PIECE_STATE) {
+                    const float4 c = sC[t + u][s];
+                    const float cc[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                    for (int j = 0; j < 4; j++) p[u] = fmaf(cc[j], h[j], p[u]);
+                }
+            }
+            if (MODE != SCAN_PIECE_STATE) {
+                float y[4];
+                reduce_rows<S>(p, s, y);
+                if constexpr (S >= 4) {
+                    if (s < 4) dtx[t + s][ch].x = y[0];
+                } else if constexpr (S == 2) {
+                    dtx[t + s][ch].x = y[0];
+                    dtx[t + 2 + s][ch].x = y[1];
+                } else {
+#pragma unroll
+                    for (int u = 0; u < 4; u++) dtx[t + u][ch].x = y[u];
+                }
+            }
+        }
+        __syncthreads();
+        if (MODE != SCAN_PIECE_STATE && n > 0) {
+            float y[PPT];
+#pragma unroll
+            for (int j = 0; j < PPT; j++) {
+                y[j] = dtx[vrow][vch + j].x;
+                if (a.D) y[j] = fmaf(Dx[j], (float)cx[j], y[j]);
+                if (a.z) y[j] *= silu((float)cz[j]);
+            }
+            store_row<PPT>(op + (int64_t)(r + vrow) * a.os, n, y);
+        }
+        // the places a thread reads here are the ones it writes for the next tile, and B and C are done with
+    }
+    if (ch >= cn) return;
+    if (MODE == SCAN_PIECE_STATE) {
+        store_row<4>(a.ws_state + unit * plane + state_at, nv, h);
+        if (s == 0) a.ws_sum[(int64_t)unit * a.channels + d] = total;
+    } else if (piece == pieces - 1) {
+        const int32_t slot = a.state ? seq_slot(a.seq, a.seq.to, i) : -1;
+        if (slot >= 0) store_row<4>(a.state + slot * a.slot_stride + state_at, nv, h);
+    }
+}
+
+// One row per sequence: the state is read and written once, which is what bounds it.
+template <typename T, int S>
+__global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
+{
+    constexpr int CW = 256 / S;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int32_t tiles = (a.channels + CW - 1) / CW;
+    const int32_t tile = (int32_t)(blockIdx.x % tiles), i = (int32_t)(blockIdx.x / tiles);
+    if (seq_end(a.seq, i, i) == i) return;
+    int s, wch;
+    lane_place<S>(lane, &s, &wch);
+    const int32_t d = tile * CW + (tid >> 6) * (64 / S) + wch;
+    if (d >= a.channels) return;                      // whole channels, so whole exchange partners
+    const int nv = a.states - 4 * s < 0 ? 0 : (a.states - 4 * s < 4 ? a.states - 4 * s : 4);
+    const int64_t state_at = (int64_t)d * a.states + 4 * s, bc = (int64_t)(d / a.per_group) * a.states + 4 * s;
+    const int32_t src = a.state ? seq_slot(a.seq, a.seq.from, i) : -1, dst = a.state ? seq_slot(a.seq, a.seq.to, i) : -1;
+
+    float A[4], h[4] = {0.0f, 0.0f, 0.0f, 0.0f}, b[4], c[4];
+    if (src >= 0) load_states(a.state + src * a.slot_stride + state_at, nv, h);
+    load_states(a.A + state_at, nv, A);
+    load_row<4>((const T*)a.B + i * a.bs + bc, nv, b);
+    load_row<4>((const T*)a.C + i * a.cs + bc, nv, c);
+    const float x = (float)((const T*)a.x)[i * a.xs + d];
+    float dt = (float)((const T*)a.dt)[i * a.dts + d] + (a.dtb ? a.dtb[d] : 0.0f);
+    if (a.softplus) dt = softplus(dt);
+    float y = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        h[j] = fmaf(__builtin_amdgcn_exp2f(dt * A[j] * kLog2e), h[j], dt * x * b[j]);
+        if (j < nv) y = fmaf(c[j], h[j], y);
+    }
+    if (dst >= 0) store_row<4>(a.state + dst * a.slot_stride + state_at, nv, h);
+    if (S >= 2) y += dpp<kXor1>(y);
+    if (S >= 4) y += dpp<kXor2>(y);
+    if (S == 16) y += dpp<kRotate4>(y);
+    if (S >= 8) y += dpp<kRotate8>(y);
+    if (s == 0) {
+        if (a.D) y = fmaf(a.D[d], x, y);
+        if (a.z) y *= silu((float)((const T*)a.z)[i * a.zs + d]);
+        ((T*)a.out)[i * a.os + d] = (T)y;
+    }
+}
+
+// Lanes per channel: 4 states each.
+static int lanes_per_channel(int states)
+{
+    int s = 1;
+    while (4 * s < states) s *= 2;
+    return s;
+}
+
+static bool is_step(const icv_sequences* seq) { return !seq->start && seq->tokens == seq->count; }
+
+// Rows per piece of a sequence, 0 where sequences stay whole.
+static int32_t piece_rows(const icv_scan_params* p, const icv_sequences* seq, int S)
+{
+    if (is_step(seq)) return 0;
+    const int cw = 256 / S, tt = 8 * S < 64 ? 8 * S : 64, per_group = p->channels / p->groups;
+    const int64_t wgs = (int64_t)p->groups * ((per_group + cw - 1) / cw) * seq->count;
+    const int64_t mean = seq->tokens / seq->count;
+    if (wgs >= 256 || mean < 512) return 0;
+    const int64_t pieces = (512 + wgs - 1) / wgs;
+    int64_t rows = (mean + pieces - 1) / pieces;
+    if (rows < 256) rows = 256;
+    return (int32_t)((rows + tt - 1) / tt * tt);
+}
+
+static int64_t piece_count(const icv_sequences* seq, int32_t rows) { return (int64_t)seq->tokens / rows + seq->count; }
+
+template <typename T, int S>
+static int launch(const ScanArgs& a, bool step, int64_t pieces, hipStream_t s)
+{
+    constexpr int CW = 256 / S;
+    const bool pad = a.states != 4 * S;
+    if (step) {
+        const int64_t n = (int64_t)((a.channels + CW - 1) / CW) * a.seq.count;
+        if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
+        k_scan_step<T, S><<<(uint32_t)n, 256, 0, s>>>(a);
+        ICV_HIP_CHECK(hipGetLastError());
+        return ICV_OK;
+    }
+    const int64_t n = (int64_t)a.group_tiles * (a.channels / a.per_group) * (a.chunk ? pieces : a.seq.count);
+    if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
+    if (!a.chunk) {
+        if (pad) k_scan<T, S, true, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
+        else k_scan<T, S, false, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
+        ICV_HIP_CHECK(hipGetLastError());
+        return ICV_OK;
+    }
+    if (pad) k_scan<T, S, true, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
+    else k_scan<T, S, false, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
+    ICV_HIP_CHECK(hipGetLastError());
+    if (pad) k_scan<T, S, true, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
+    else k_scan<T, S, false, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
+    ICV_HIP_CHECK(hipGetLastError());
+    return ICV_OK;
+}
+
+template <typename T>
+static int launch_lanes(const ScanArgs& a, int S, bool step, int64_t pieces, hipStream_t s)
+{
+    switch (S) {
+        case 1: return launch<T, 1>(a, step, pieces, s);
+        case 2: return launch<T, 2>(a, step, pieces, s);
+        case 4: return launch<T, 4>(a, step, pieces, s);
+        case 8: return launch<T, 8>(a, step, pieces, s);
+        default: return launch<T, 16>(a, step, pieces, s);
+    }
+}
+
+static int check_scan(const icv_scan_params* p, const icv_sequences* seq, SeqArgs* sa)
+{
+    if (!p || p->channels < 1 || p->states < 1 || p->groups < 1 || p->channels % p->groups != 0) return ICV_ERR_INVALID_ARG;
+    if (p->states > 64) return ICV_ERR_UNSUPPORTED;
+    if (p->softplus != 0 && p->softplus != 1) return ICV_ERR_INVALID_ARG;
+    if (p->dtype == ICV_U8I8) return ICV_ERR_UNSUPPORTED;
+    if (p->dtype != ICV_F32 && p->dtype != ICV_BF16) return ICV_ERR_INVALID_ARG;
+    for (int32_t r : {p->x_row_stride, p->dt_row_stride, p->z_row_stride, p->out_row_stride})
+        if (r && r < p->channels) return ICV_ERR_INVALID_ARG;
+    for (int32_t r : {p->b_row_stride, p->c_row_stride})
+        if (r && r < (int64_t)p->groups * p->states) return ICV_ERR_INVALID_ARG;
+    if (p->state_slots < 0 || (p->state_slot_stride && p->state_slot_stride < (int64_t)p->channels * p->states))
+        return ICV_ERR_INVALID_ARG;
+    return make_seq_args(seq, p->state_slots, sa);
+}
+
+}  // namespace icv
+
+extern "C" size_t icv_selective_scan_workspace_bytes(const icv_scan_params* p, const icv_sequences* seq)
+{
+    using namespace icv;
+    SeqArgs sa;
+    if (check_scan(p, seq, &sa) != ICV_OK || seq->count == 0 || seq->tokens == 0) return 0;
+    const int32_t rows = piece_rows(p, seq, lanes_per_channel(p->states));
+    if (!rows) return 0;
+    return (size_t)piece_count(seq, rows) * p->channels * (p->states + 1) * sizeof(float);
+}
+
+extern "C" int icv_selective_scan(const icv_scan_params* p, const icv_sequences* seq, const icv_scan_tensors* t,
+                                  void* workspace, void* stream)
+{
+    using namespace icv;
+    ScanArgs a;
+    const int st = check_scan(p, seq, &a.seq);
+    if (st != ICV_OK) return st;
+    if (!t) return ICV_ERR_INVALID_ARG;
+    if (seq->count == 0 || seq->tokens == 0) return ICV_OK;
+    if (!t->x || !t->dt || !t->A || !t->B || !t->C || !t->out) return ICV_ERR_INVALID_ARG;
+    const uintptr_t size = p->dtype == ICV_F32 ? 4 : 2;
+    for (const void* q : {t->x, t->dt, t->B, t->C, t->z, (const void*)t->out})
+        if (misaligned(q, size)) return ICV_ERR_INVALID_ARG;
+    for (const void* q : {(const void*)t->A, (const void*)t->D, (const void*)t->dt_bias, (const void*)t->state})
+        if (misaligned(q, 4)) return ICV_ERR_INVALID_ARG;
+    const auto stride = [](int32_t s, int64_t dense) { return s ? (int64_t)s : dense; };
+    a.x = t->x; a.dt = t->dt; a.B = t->B; a.C = t->C; a.z = t->z;
+    a.A = t->A; a.D = t->D; a.dtb = t->dt_bias; a.state = t->state; a.out = t->out;
+    a.xs = stride(p->x_row_stride, p->channels);
+    a.dts = stride(p->dt_row_stride, p->channels);
+    a.zs = stride(p->z_row_stride, p->channels);
+    a.os = stride(p->out_row_stride, p->channels);
+    a.bs = stride(p->b_row_stride, (int64_t)p->groups * p->states);
+    a.cs = stride(p->c_row_stride, (int64_t)p->groups * p->states);
+    // an output over an input: an element is read before it is written, by the same thread, if both lie at the same place
+    if ((a.out == a.x && a.os != a.xs) || (a.out == a.dt && a.os != a.dts) || (a.out == a.z && a.os != a.zs) ||
+        a.out == a.B || a.out == a.C)
+        return ICV_ERR_INVALID_ARG;
+    a.slot_stride = p->state_slot_stride ? p->state_slot_stride : (int64_t)p->channels * p->states;
+    a.channels = p->channels; a.states = p->states; a.per_group = p->channels / p->groups; a.softplus = p->softplus;
+    const int S = lanes_per_channel(p->states), cw = 256 / S;
+    a.group_tiles = (a.per_group + cw - 1) / cw;
+    a.chunk = piece_rows(p, seq, S);
+    const int64_t pieces = a.chunk ? piece_count(seq, a.chunk) : 0;
+    if (a.chunk && (!workspace || misaligned(workspace, 16))) return ICV_ERR_INVALID_ARG;
+    a.units = (int32_t)pieces;
+    a.ws_state = (float*)workspace;
+    a.ws_sum = a.ws_state + pieces * a.channels * a.states;
+    hipStream_t s = (hipStream_t)stream;
+    return p->dtype == ICV_F32 ? launch_lanes<float>(a, S, is_step(seq), pieces, s)
+                               : launch_lanes<__bf16>(a, S, is_step(seq), pieces, s);
+}

@@ -1,0 +1,91 @@
+// What the operators on sequences share: which rows belong to a sequence (icv_sequences), rows of any alignment, the
+// activations.
+#pragma once
+#include "icv_internal.h"
+
+namespace icv {
+
+// icv_sequences as the kernels see it; `each` is the rows per sequence without a start array.
+struct SeqArgs {
+    int32_t count, tokens, each;
+    const int32_t* start;
+    const int32_t* length;
+    const int32_t* from;
+    const int32_t* to;
+    int32_t slots;
+};
+
+inline int make_seq_args(const icv_sequences* s, int32_t slots, SeqArgs* a)
+{
+    if (!s || s->count < 0 || s->tokens < 0) return ICV_ERR_INVALID_ARG;
+    if (!s->start && s->count > 0 && s->tokens % s->count != 0) return ICV_ERR_INVALID_ARG;
+    for (const int32_t* q : {s->start, s->length, s->from, s->to})
+        if ((uintptr_t)q & 3u) return ICV_ERR_INVALID_ARG;
+    *a = {s->count, s->tokens, s->count > 0 ? s->tokens / s->count : 0, s->start, s->length, s->from, s->to, slots};
+    return ICV_OK;
+}
+
+inline bool misaligned(const void* p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
+
+__device__ inline int32_t clamp_row(int32_t v, int32_t tokens) { return v < 0 ? 0 : (v > tokens ? tokens : v); }
+
+// Row of the first of sequence i's rows; i = count gives the end of the last one's.
+__device__ inline int32_t seq_begin(const SeqArgs& s, int32_t i)
+{
+    return s.start ? clamp_row(s.start[i], s.tokens) : i * s.each;
+}
+
+// One past sequence i's last row: its length's worth of the rows up to the next sequence, never before `begin`.
+__device__ inline int32_t seq_end(const SeqArgs& s, int32_t i, int32_t begin)
+{
+    int32_t n = seq_begin(s, i + 1) - begin;
+    if (s.length && s.length[i] < n) n = s.length[i];
+    return begin + (n > 0 ? n : 0);
+}
+
+// The slot a sequence continues or leaves its state in; -1: none.
+__device__ inline int32_t seq_slot(const SeqArgs& s, const int32_t* which, int32_t i)
+{
+    const int32_t v = which ? which[i] : i;
+    return v >= 0 && v < s.slots ? v : -1;
+}
+
+template <typename T>
+__device__ inline float to_float(T v) { return (float)v; }
+
+// N elements from any address of the element's own alignment (one wide load: global memory takes any address),
+// `n` < N of them where a row ends; the rest read as zero.
+template <int N, typename T>
+__device__ inline void load_row(const T* p, int n, float (&v)[N])
+{
+    if (n >= N) {
+        T r[N];
+        __builtin_memcpy(r, p, sizeof(r));
+#pragma unroll
+        for (int j = 0; j < N; j++) v[j] = (float)r[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; j++) v[j] = j < n ? (float)p[j] : 0.0f;
+    }
+}
+
+template <int N, typename T>
+__device__ inline void store_row(T* p, int n, const float (&v)[N])
+{
+    if (n >= N) {
+        T r[N];
+#pragma unroll
+        for (int j = 0; j < N; j++) r[j] = (T)v[j];
+        __builtin_memcpy(p, r, sizeof(r));
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; j++)
+            if (j < n) p[j] = (T)v[j];
+    }
+}
+
+// v / (1 + exp(-v)).  exp(-v) overflows to infinity below -88, which gives -0, the limit; the reciprocal is the
+// hardware's, within 1 ulp, next to an output rounding of at least that.
+__device__ inline float silu(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f)); }
+
+}  // namespace icv

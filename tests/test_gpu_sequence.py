@@ -1,0 +1,413 @@
+"""The operators on sequences on the GPU against their definitions in 64 bits (sequence_reference)."""
+import pytest
+import torch
+
+import sequence_reference as ref
+from paper_1907_02129_amd import binding as icv
+
+pytestmark = pytest.mark.gpu
+TYPE = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+def ints(v):
+    return None if v is None else torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def wide(t, pad, before=0):
+    """The same matrix on the device as a slice of a wider one whose other columns hold NaN."""
+    if not pad and not before:
+        return t.cuda()
+    full = torch.full((t.shape[0], t.shape[1] + pad + before), float("nan"), dtype=t.dtype)
+    full[:, before:before + t.shape[1]] = t
+    return full.cuda()[:, before:before + t.shape[1]]
+
+
+class Batch:
+    """Sequences of given lengths in `tokens` rows.  layout: "packed" (one behind the other, rows behind the last
+    belong to none), "padded" (each in a room of the same size), "step" (one row each)."""
+
+    def __init__(self, lengths, layout="packed", tail=0, source=None, target=None, slots=None):
+        self.count = len(lengths)
+        self.start = self.length = None
+        if layout == "packed":
+            at = [0]
+            for n in lengths:
+                at.append(at[-1] + n)
+            self.start, self.tokens = at, at[-1] + tail
+        elif layout == "padded":
+            room = max(max(lengths), 1) + tail
+            self.tokens, self.length = room * self.count, list(lengths)
+        else:
+            self.tokens, self.length = self.count, None if all(lengths) else list(lengths)
+        self.rows = ref.spans(self.count, self.tokens, self.start, self.length)
+        self.slots = slots or self.count
+        self.source, self.target = source, target
+        self.from_ = source if source is not None else list(range(self.count))
+        self.to = target if target is not None else list(range(self.count))
+
+    def seq(self):
+        return icv.make_sequences(self.count, self.tokens, ints(self.start), ints(self.length), ints(self.source), ints(self.target))
+
+    def inside(self):
+        keep = torch.zeros(self.tokens, dtype=torch.bool)
+        for b, n in self.rows:
+            keep[b:b + n] = True
+        return keep
+
+
+BATCHES = {
+    "one_row": Batch([1], "step"),
+    "steps": Batch([1] * 9, "step", source=[3, -1, 0, 1, 2, 99, 6, 7, 8], target=[9, 10, 11, 12, -1, 13, 6, 7, 99], slots=14),
+    "steps_some_idle": Batch([1, 0, 1, 1, 0], "step"),
+    "packed": Batch([5, 0, 1, 70, 2, 0, 33], "packed", tail=3, source=[0, 1, -1, 3, 4, 5, 0], target=[7, 8, 2, 3, 4, 5, -5], slots=9),
+    "padded": Batch([17, 0, 64, 1, 3], "padded", tail=2),
+    "one_long": Batch([517]),
+    "short_ones": Batch([1, 2, 3, 1, 1, 2, 3, 4, 1, 1, 0, 0, 5, 1, 2], "packed"),
+    "nothing": Batch([0, 0], "packed", tail=5),
+}
+
+
+def conv_case(batch, channels, taps, dtype, silu, bias, state, pad, seed):
+    g, t = gen(seed), TYPE[dtype]
+    x = torch.randn(batch.tokens, channels, generator=g).to(t)
+    keep = batch.inside()
+    x[~keep] = float("nan")                      # nothing of these rows may be read
+    filt = torch.randn(channels, taps, generator=g).to(t)
+    b = torch.randn(channels, generator=g) if bias else None
+    st = torch.randn(batch.slots, taps - 1, channels, generator=g).to(t)
+    out = torch.randn(batch.tokens, channels, generator=g).to(t)
+    p = icv.make_causal_conv_params(channels, taps, dtype, silu, in_row_stride=channels + 2 * pad, out_row_stride=channels + pad,
+                                    state_slots=batch.slots if state else 0)
+    std, outd = st.cuda(), wide(out, pad)
+    icv.causal_conv1d(p, batch.seq(), wide(x, pad, pad), filt.cuda(), None if b is None else b.cuda(), std if state else None, outd)
+    torch.cuda.synchronize()
+    none = [-1] * batch.count
+    want, bound, st_want = ref.causal_conv(x, filt, b, st, batch.rows, batch.from_ if state else none, batch.to if state else none,
+                                           silu, out, t)
+    ref.check("out", outd, want, bound)
+    assert torch.equal(std.cpu().double(), st_want)
+    assert torch.equal(outd.cpu()[~keep], out[~keep])
+
+
+@pytest.mark.parametrize("name", list(BATCHES))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_causal_conv_batches(name, dtype):
+    conv_case(BATCHES[name], 72, 4, dtype, True, True, True, 0, 1)
+
+
+@pytest.mark.parametrize("taps", range(1, 9))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_causal_conv_taps(taps, dtype):
+    for name in ("packed", "padded", "short_ones", "steps"):
+        conv_case(BATCHES[name], 24, taps, dtype, False, True, True, 1, taps)
+
+
+@pytest.mark.parametrize("channels", [1, 7, 8, 9, 63, 130, 515, 2056])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_causal_conv_widths_and_alignments(channels, dtype):
+    conv_case(BATCHES["packed"], channels, 4, dtype, True, False, True, 3, channels)
+    conv_case(BATCHES["one_long"], channels, 3, dtype, True, True, False, 0, channels)
+
+
+def scan_case(batch, channels, states, groups, dtype, softplus, extras, state, pad, seed, scale=1.0):
+    g, t = gen(seed), TYPE[dtype]
+    keep, n = batch.inside(), batch.tokens
+
+    def rows(width):
+        v = torch.randn(n, width, generator=g).to(t)
+        v[~keep] = float("nan")
+        return v
+
+    x, B, C = rows(channels), rows(groups * states), rows(groups * states)
+    dt = (rows(channels).float() * (1.0 if softplus else 0.02)).to(t)
+    if not softplus:
+        dt = dt.abs()
+    A = -(torch.rand(channels, states, generator=g) * states + 0.1) * scale
+    D = torch.randn(channels, generator=g) if extras else None
+    bias = torch.rand(channels, generator=g) * 5 - 6 if extras else None
+    z = rows(channels) if extras else None
+    st = torch.randn(batch.slots, channels, states, generator=g)
+    out = torch.randn(n, channels, generator=g).to(t)
+    bc = groups * states
+    p = icv.make_scan_params(channels, states, dtype, groups, softplus, channels + pad, channels + 2 * pad, bc + 3 * pad, bc + pad,
+                             channels + pad, channels + 2 * pad, batch.slots if state else 0)
+    seq, std, outd = batch.seq(), st.cuda(), wide(out, 2 * pad)
+    dev = lambda v: None if v is None else v.cuda()  # noqa: E731
+    space = icv.selective_scan_workspace_bytes(p, seq)
+    ws = torch.full((space // 4,), float("nan"), device="cuda") if space else None
+    icv.selective_scan(p, seq, wide(x, pad), wide(dt, pad, pad), A.cuda(), wide(B, 2 * pad, pad), wide(C, pad), dev(D),
+                       None if z is None else wide(z, 0, pad), dev(bias), std if state else None, outd, ws)
+    torch.cuda.synchronize()
+    none = [-1] * batch.count
+    piece = max(n for _, n in batch.rows) if space else 0
+    want, bound, st_want, sbound = ref.selective_scan(x, dt, A, B, C, D, z, bias, st, batch.rows, batch.from_ if state else none,
+                                                      batch.to if state else none, groups, softplus, out, t, piece)
+    ref.check("out", outd, want, bound)
+    ref.check("state", std, st_want, sbound)
+    assert torch.equal(outd.cpu()[~keep], out[~keep])
+    return space
+
+
+@pytest.mark.parametrize("name", list(BATCHES))
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_selective_scan_batches(name, dtype):
+    scan_case(BATCHES[name], 72, 16, 1, dtype, True, True, True, 0, 1)
+
+
+@pytest.mark.parametrize("states", [1, 2, 3, 4, 5, 8, 13, 16, 17, 32, 41, 64])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_selective_scan_state_sizes(states, dtype):
+    for name in ("packed", "steps"):
+        scan_case(BATCHES[name], 21, states, 3, dtype, True, True, True, 1, states)
+
+
+@pytest.mark.parametrize("channels,groups", [(1, 1), (2, 2), (63, 1), (65, 5), (130, 2), (264, 4), (515, 5)])
+def test_selective_scan_widths_groups_and_alignments(channels, groups):
+    for dtype, name, extras in (("bf16", "packed", True), ("f32", "padded", False), ("bf16", "steps", False)):
+        scan_case(BATCHES[name], channels, 16, groups, dtype, extras, extras, name != "padded", 3, channels)
+
+
+@pytest.mark.parametrize("states", [4, 8, 16, 30, 64])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_selective_scan_long_sequences_in_pieces(states, dtype):
+    """Few channels and long sequences: cut into pieces that meet in the workspace.  Slow decays, so that what crosses a
+    border counts."""
+    batch = Batch([1500, 0, 257, 1, 900], "packed", tail=7, source=[2, 0, -1, 3, 4], target=[2, 5, 6, 0, 4], slots=7)
+    for b in (batch, Batch([1400]), Batch([1283, 1100], "padded", tail=3)):
+        assert scan_case(b, 20, states, 2, dtype, True, True, True, 1, states, scale=0.02) > 0
+
+
+def test_selective_scan_infinite_inputs_stay_in_their_channel():
+    """An infinite or NaN input reaches its own channel only, and one that the padding of the state must not turn into NaN."""
+    batch, ch, N = Batch([40, 3]), 33, 3
+    g = gen(5)
+    x, dt = torch.randn(43, ch, generator=g), torch.rand(43, ch, generator=g)
+    B, C = torch.rand(43, N, generator=g) + 0.5, torch.rand(43, N, generator=g) + 0.5
+    x[7, 2], x[9, 30] = float("inf"), float("nan")
+    A = -torch.rand(ch, N, generator=g) - 0.1
+    A[11, 1] = -float("inf")                    # a state that forgets everything
+    p = icv.make_scan_params(ch, N, "f32", softplus=False)
+    out = torch.empty(43, ch, device="cuda")
+    icv.selective_scan(p, batch.seq(), x.cuda(), dt.cuda(), A.cuda(), B.cuda(), C.cuda(), None, None, None, None, out)
+    want, bound, _, _ = ref.selective_scan(x, dt, A, B, C, None, None, None, torch.zeros(1, ch, N), batch.rows, [-1] * 2, [-1] * 2, 1,
+                                           False, torch.zeros(43, ch), torch.float32)
+    got = out.cpu().double()
+    assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf())
+    fine = want.isfinite() & bound.isfinite()
+    fine[:, 11] = False
+    ref.check("out", got[fine], want[fine], bound[fine])
+    assert (got[:, 11] - want[:, 11]).abs().max() <= 1e-5 * want[:, 11].abs().max()
+
+
+def test_scan_output_may_lie_over_x_dt_or_z():
+    batch, ch, N = Batch([700]), 40, 16
+    g = gen(8)
+    x, dt, z = (torch.randn(700, ch, generator=g).bfloat16().cuda() for _ in range(3))
+    B, C = (torch.randn(700, N, generator=g).bfloat16().cuda() for _ in range(2))
+    A = -torch.rand(ch, N, generator=g).cuda()
+    p = icv.make_scan_params(ch, N, "bf16")
+    seq = batch.seq()
+    ws = torch.empty(icv.selective_scan_workspace_bytes(p, seq), dtype=torch.uint8, device="cuda")
+    want = torch.empty_like(x)
+    icv.selective_scan(p, seq, x, dt, A, B, C, None, z, None, None, want, ws)
+    for k in range(3):
+        ins = [x.clone(), dt.clone(), z.clone()]
+        icv.selective_scan(p, seq, ins[0], ins[1], A, B, C, None, ins[2], None, None, ins[k], ws)
+        assert torch.equal(ins[k], want)
+
+
+def test_rows_past_32_bit_offsets():
+    """Row strides that put the last rows past 2^32 bytes, and state slots past 2^32 bytes."""
+    ch, N, stride, n = 64, 16, 1 << 20, 2100
+    batch = Batch([n - 5, 5], slots=2)
+    g = gen(9)
+    big = torch.empty(n * stride, dtype=torch.bfloat16, device="cuda")
+    x = torch.as_strided(big, (n, ch), (stride, 1), 64)
+    x.copy_(torch.randn(n, ch, generator=g))
+    filt, st = torch.randn(ch, 4, generator=g).bfloat16(), torch.zeros(2, 3, ch).bfloat16()
+    room = torch.empty((1 << 31) + 3 * ch, dtype=torch.bfloat16, device="cuda")
+    state = torch.as_strided(room, (2, 3, ch), (1 << 31, ch, 1))
+    state.zero_()
+    out = torch.as_strided(big, (n, ch), (stride, 1), 256)
+    p = icv.make_causal_conv_params(ch, 4, "bf16", True, stride, stride, 2, 1 << 31)
+    icv.causal_conv1d(p, batch.seq(), x, filt.cuda(), None, state, out)
+    xc = x.cpu()
+    want, bound, st_want = ref.causal_conv(xc, filt, None, st, batch.rows, [0, 1], [0, 1], True, torch.zeros(n, ch), torch.bfloat16)
+    ref.check("out", out, want, bound)
+    assert torch.equal(state.cpu().double(), st_want)
+
+    dt, B, C = torch.rand(n, ch, generator=g).bfloat16(), torch.randn(n, N, generator=g).bfloat16(), torch.randn(n, N, generator=g).bfloat16()
+    A = -torch.rand(ch, N, generator=g) - 0.1
+    state = torch.as_strided(room.view(torch.float32), (2, ch, N), ((1 << 30) - 1024, N, 1))
+    state.zero_()
+    p = icv.make_scan_params(ch, N, "bf16", 1, False, x_row_stride=stride, out_row_stride=stride, state_slots=2,
+                             state_slot_stride=(1 << 30) - 1024)
+    seq = batch.seq()
+    ws = torch.empty(icv.selective_scan_workspace_bytes(p, seq), dtype=torch.uint8, device="cuda")
+    icv.selective_scan(p, seq, x, dt.cuda(), A.cuda(), B.cuda(), C.cuda(), None, None, None, state, out, ws)
+    want, bound, st_want, sbound = ref.selective_scan(xc, dt, A, B, C, None, None, None, torch.zeros(2, ch, N), batch.rows, [0, 1], [0, 1],
+                                                      1, False, torch.zeros(n, ch), torch.bfloat16, n)
+    ref.check("out", out, want, bound)
+    ref.check("state", state, st_want, sbound)
+
+
+def test_arrays_out_of_range_lead_nowhere():
+    """Start values out of range or decreasing, lengths and slots out of range: rows and slots outside stay as they are."""
+    ch, N = 24, 16
+    tokens, guard = 1600, 64
+    g = gen(10)
+    x = torch.randn(tokens, ch, generator=g).bfloat16().cuda()
+    filt, A = torch.randn(ch, 4, generator=g).bfloat16().cuda(), -torch.rand(ch, N, generator=g).cuda()
+    B = torch.randn(tokens, N, generator=g).bfloat16().cuda()
+    for start in ([-5, 300, 10_000], [500, 100, 1600], [0, 1600, 0], [1700, 1800, 1900], [-9, -8, -7], [0, 1600, 0, 1600]):
+        n = len(start) - 1
+        seq = icv.make_sequences(n, tokens, ints(start), ints([10 ** 9, 2 ** 31 - 1, 10 ** 9][:n]), ints([2 ** 31 - 1, -7, 2][:n]),
+                                 ints([-2 ** 31, 2, -1][:n]))
+        full = torch.full((tokens + 2 * guard, ch), 7.0, dtype=torch.bfloat16, device="cuda")
+        conv_state = torch.full((2, 3, ch), 5.0, dtype=torch.bfloat16, device="cuda")
+        scan_state = torch.full((2, ch, N), 5.0, device="cuda")
+        out = full[guard:guard + tokens]
+        icv.causal_conv1d(icv.make_causal_conv_params(ch, 4, "bf16", state_slots=2), seq, x, filt, None, conv_state, out)
+        p = icv.make_scan_params(ch, N, "bf16", state_slots=2)
+        space = icv.selective_scan_workspace_bytes(p, seq)
+        assert space > 0
+        ws = torch.full((space + 4096,), 99, dtype=torch.uint8, device="cuda")
+        icv.selective_scan(p, seq, x, x, A, B, B, None, None, None, scan_state, out, ws)
+        torch.cuda.synchronize()
+        assert (full[:guard] == 7).all() and (full[guard + tokens:] == 7).all()
+        assert (conv_state == 5).all() and (scan_state == 5).all() and (ws[space:] == 99).all()
+
+
+def test_many_short_sequences_and_many_slots():
+    batch = Batch([(i * 7) % 5 for i in range(400)], "packed", source=[(i * 3) % 400 for i in range(400)],
+                  target=[400 + i for i in range(400)], slots=800)
+    conv_case(batch, 40, 4, "bf16", True, True, True, 0, 11)
+    scan_case(batch, 40, 16, 1, "bf16", True, True, True, 0, 11)
+
+
+def test_prompt_then_single_tokens_in_a_replayed_graph():
+    """A prompt in one call, then single tokens from a captured graph of both operators, the state in place: the states and
+    outputs are those of the whole sequence in 64 bits at every replay.  Eager calls and slot changes come in between."""
+    ch, N, W, prompt, more, count = 48, 16, 4, 29, 6, 3
+    g = gen(12)
+    total = prompt + more
+    x = torch.randn(count, total, ch, generator=g)
+    dt = torch.randn(count, total, ch, generator=g)
+    B, C = torch.randn(count, total, N, generator=g), torch.randn(count, total, N, generator=g)
+    filt, A = torch.randn(ch, W, generator=g), -torch.rand(ch, N, generator=g) - 0.1
+    dev = lambda v: v.cuda().contiguous()  # noqa: E731
+    cs, ss = torch.full((5, W - 1, ch), 9.0, device="cuda"), torch.full((5, ch, N), 9.0, device="cuda")
+    pc, ps = icv.make_causal_conv_params(ch, W, "f32", state_slots=5), icv.make_scan_params(ch, N, "f32", state_slots=5)
+    fd, Ad = dev(filt), dev(A)
+    first = icv.make_sequences(count, count * prompt, None, None, ints([-1] * count), ints([4, 0, 2]))
+    u, y = torch.empty(count * prompt, ch, device="cuda"), torch.empty(count * prompt, ch, device="cuda")
+    cut = lambda v: dev(v[:, :prompt].reshape(count * prompt, -1))  # noqa: E731
+    icv.causal_conv1d(pc, first, cut(x), fd, None, cs, u)
+    icv.selective_scan(ps, first, u, cut(dt), Ad, cut(B), cut(C), None, None, None, ss, y)
+
+    slots = ints([4, 0, 2])
+    step = icv.make_sequences(count, count, None, None, slots, slots)
+    xs, dts, Bs, Cs = (torch.zeros(count, w, device="cuda") for w in (ch, ch, N, N))
+    us, ys = torch.zeros(count, ch, device="cuda"), torch.zeros(count, ch, device="cuda")
+
+    def one():
+        icv.causal_conv1d(pc, step, xs, fd, None, cs, us)
+        icv.selective_scan(ps, step, us, dts, Ad, Bs, Cs, None, None, None, ss, ys)
+
+    kept = cs.clone(), ss.clone()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        one()
+    side.synchronize()
+    cs.copy_(kept[0]), ss.copy_(kept[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        one()
+    none = [-1] * count
+    rows = [(i * total, total) for i in range(count)]
+    flat = lambda v: v.reshape(count * total, -1)  # noqa: E731
+    uw, ub, _ = ref.causal_conv(flat(x), filt, None, torch.zeros(1, W - 1, ch), rows, none, none, True, torch.zeros(count * total, ch), torch.float32)
+    # the scan's own bound, and what the convolution's may add: the scan is linear in x, so it takes the bound through |B|, |C|
+    yw, yb, _, _ = ref.selective_scan(uw, flat(dt), A, flat(B), flat(C), None, None, None, torch.zeros(1, ch, N), rows, none, none, 1, True,
+                                      torch.zeros(count * total, ch), torch.float32)
+    more_b, _, _, _ = ref.selective_scan(ub, flat(dt), A, flat(B).abs(), flat(C).abs(), None, None, None, torch.zeros(1, ch, N), rows, none,
+                                         none, 1, True, torch.zeros(count * total, ch), torch.float32)
+    place = lambda v: v.view(count, total, ch)  # noqa: E731
+    ref.check("prompt", y.view(count, prompt, ch), place(yw)[:, :prompt], place(yb + more_b)[:, :prompt])
+    order = [4, 0, 2]
+    for k in range(more):
+        for d, s in ((xs, x), (dts, dt), (Bs, B), (Cs, C)):
+            d.copy_(s[:, prompt + k])
+        if k == 3:                              # the server moves the states of two sequences
+            cs[[1, 3]], ss[[1, 3]] = cs[[4, 0]], ss[[4, 0]]
+            slots.copy_(ints([1, 3, 2]))
+        graph.replay()
+        torch.cuda.synchronize()
+        ref.check("step", ys, place(yw)[:, prompt + k], place(yb + more_b)[:, prompt + k])
+        torch.randn(1000, device="cuda").sum()
+
+
+def test_captured_prompt_in_pieces_replays():
+    """A prompt that is cut into pieces, captured; replays follow new inputs and new starts."""
+    ch, N, tokens = 32, 16, 1600
+    g = gen(13)
+    make = lambda w: torch.randn(tokens, w, generator=g)  # noqa: E731
+    A = -0.02 * torch.rand(ch, N, generator=g) - 0.001
+    x, dt, B, C = (v.bfloat16().cuda() for v in (make(ch), make(ch), make(N), make(N)))
+    start = ints([0, 1000, 1600])
+    seq = icv.make_sequences(2, tokens, start)
+    p = icv.make_scan_params(ch, N, "bf16", state_slots=2)
+    ws = torch.empty(icv.selective_scan_workspace_bytes(p, seq), dtype=torch.uint8, device="cuda")
+    assert ws.numel() > 0
+    state, out, Ad = torch.zeros(2, ch, N, device="cuda"), torch.zeros(tokens, ch, dtype=torch.bfloat16, device="cuda"), A.cuda()
+
+    def go():
+        icv.selective_scan(p, seq, x, dt, Ad, B, C, None, None, None, state, out, ws)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        go()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for at in (1000, 40, 1599, 0):
+        x.copy_(make(ch))
+        start.copy_(ints([0, at, tokens]))
+        state.zero_()
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_state = out.clone(), state.clone()
+        want, bound, sw, sb = ref.selective_scan(x.cpu(), dt.cpu(), A, B.cpu(), C.cpu(), None, None, None, torch.zeros(2, ch, N),
+                                                 [(0, at), (at, tokens - at)], [0, 1], [0, 1], 1, True, torch.zeros(tokens, ch),
+                                                 torch.bfloat16, tokens)
+        ref.check("out", got, want, bound)
+        ref.check("state", got_state, sw, sb)
+        state.zero_()
+        go()
+        assert torch.equal(out, got) and torch.equal(state, got_state)
+
+
+def test_calls_on_a_stream_of_their_own():
+    ch, N = 64, 16
+    batch = BATCHES["packed"]
+    g = gen(14)
+    x = torch.randn(batch.tokens, ch, generator=g).bfloat16().cuda()
+    B = torch.randn(batch.tokens, N, generator=g).bfloat16().cuda()
+    filt, A = torch.randn(ch, 4, generator=g).bfloat16().cuda(), -torch.rand(ch, N, generator=g).cuda()
+    pc, ps = icv.make_causal_conv_params(ch, 4), icv.make_scan_params(ch, N)
+    results = []
+    torch.cuda.synchronize()
+    for stream in (None, torch.cuda.Stream()):
+        u, y = torch.zeros_like(x), torch.zeros_like(x)
+        torch.cuda.synchronize()
+        icv.causal_conv1d(pc, batch.seq(), x, filt, None, None, u, stream=stream)
+        icv.selective_scan(ps, batch.seq(), u, x, A, B, B, None, x, None, None, y, stream=stream)
+        torch.cuda.synchronize()
+        results.append((u, y))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
