@@ -4,14 +4,14 @@
 // products run on the tensor cores, one 16 x 16 x 128 instruction per block; a block's sum is scaled and added to the
 // float accumulator on the vector ALU, one multiply-add per output and block (the two scales' product is the same for
 // the 4 outputs that a lane holds, which are neighbouring columns of one row).
-#include "icv_internal.h"
+#include "icv_mfma_common.h"
+#include <cmath>
 
 namespace icv {
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 struct MatmulArgs {
     const uint8_t *a, *b;
@@ -19,6 +19,7 @@ struct MatmulArgs {
     void* out;
     int32_t rows, cols, blocks, col_blocks;
     int64_t as, bs, os;
+    uint32_t col_tiles, row_tiles, tiles, per_xcd;      // of the tile kernel
 };
 
 // Eight codes as bfloat16.
@@ -38,18 +39,33 @@ __device__ inline bf16x8_t widen(int lo, int hi)
 // result, far below a bfloat16 output's rounding (2^-9) but not below a float's.  EXACT, for float outputs, widens the codes to bfloat16
 // (no rounding) and uses that type's instruction, whose products and sums are float's, at half the rate.
 template <bool EXACT>
-__device__ inline f32x4_t block_product(i32x8_t b, i32x8_t a)
-{
-    const f32x4_t zero = {0.0f, 0.0f, 0.0f, 0.0f};
-    if constexpr (!EXACT) {
-        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b, a, zero, 0, 0, 0, 0, 0, 0);
-    } else {
-        f32x4_t c = zero;
+struct Operand;
+template <>
+struct Operand<false> {
+    i32x8_t v;
+    __device__ void set(i32x8_t codes) { v = codes; }
+};
+template <>
+struct Operand<true> {
+    bf16x8_t v[4];
+    __device__ void set(i32x8_t codes)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; i++)
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(b[2 * i], b[2 * i + 1]), widen(a[2 * i], a[2 * i + 1]), c, 0, 0, 0);
-        return c;
+        for (int i = 0; i < 4; i++) v[i] = widen(codes[2 * i], codes[2 * i + 1]);
     }
+};
+
+template <bool EXACT>
+__device__ inline f32x4_t block_product(const Operand<EXACT>& b, const Operand<EXACT>& a)
+{
+    f32x4_t c = {0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (!EXACT) {
+        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.v, a.v, c, 0, 0, 0, 0, 0, 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.v[i], a.v[i], c, 0, 0, 0);
+    }
+    return c;
 }
 
 // 32 of the 128 codes at `row`: 16 from each half, so that the 4 lanes of a row read 64 bytes side by side.
@@ -68,57 +84,371 @@ __device__ inline void store_out(const MatmulArgs& g, int64_t m, int32_t n, f32x
         if (n + j < g.cols) o[j] = (OUT)(v[j] + (g.bias ? g.bias[n + j] : 0.0f));
 }
 
-// 16 columns x 16 * MB rows per workgroup, the blocks of the reduction dealt to its wavefronts, whose sums meet in LDS.
-template <typename OUT, int MB, int WAVES>
+// 16 columns x 16 rows per workgroup, the blocks of the reduction dealt to its wavefronts, whose sums meet in LDS.
+// For few rows, where reading b is all there is: a wavefront has the codes of two blocks on their way at once (four: 8 x 4096,
+// 2048 deep 6.0 us instead of 5.9).
+template <typename OUT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_matmul_split(MatmulArgs g)
 {
-    __shared__ f32x4_t part[WAVES][MB][64];
+    constexpr bool EXACT = std::is_same<OUT, float>::value;
+    constexpr int DEPTH = 2;
+    __shared__ f32x4_t part[WAVES][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, quarter = lane >> 4;
     const int32_t col_tiles = (g.cols + 15) / 16;
     const int32_t n0 = (int32_t)(blockIdx.x % col_tiles) * 16;
-    const int64_t m0 = (int64_t)(blockIdx.x / col_tiles) * (16 * MB);
+    const int64_t m0 = (int64_t)(blockIdx.x / col_tiles) * 16;
+    const int64_t m = m0 + row < g.rows ? m0 + row : g.rows - 1;      // rows past the end repeat the last
     const uint8_t* bp = g.b + (int64_t)(n0 + row < g.cols ? n0 + row : g.cols - 1) * g.bs;
-    const uint8_t* ap[MB];
-    int64_t m[MB];
+    const uint8_t* ap = g.a + m * g.as;
+    const float *sb = g.sb + n0 / 128, *sa = g.sa + m;
+    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int32_t k0 = wave; k0 < g.blocks; k0 += DEPTH * WAVES) {
+        i32x8_t bc[DEPTH], ac[DEPTH];
+        float scale[DEPTH];
 #pragma unroll
-    for (int i = 0; i < MB; i++) {
-        m[i] = m0 + 16 * i + row < g.rows ? m0 + 16 * i + row : g.rows - 1;      // rows past the end repeat the last
-        ap[i] = g.a + m[i] * g.as;
-    }
-    f32x4_t acc[MB];
+        for (int d = 0; d < DEPTH; d++) {
+            // blocks past the end repeat the first of these and count nothing
+            const int64_t k = k0 + d * WAVES < g.blocks ? k0 + d * WAVES : k0;
+            bc[d] = load_codes(bp + k * 128, quarter);
+            ac[d] = load_codes(ap + k * 128, quarter);
+            scale[d] = sb[k * g.col_blocks] * sa[k * g.rows];
+        }
 #pragma unroll
-    for (int i = 0; i < MB; i++) acc[i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int32_t k = wave; k < g.blocks; k += WAVES) {
-        const i32x8_t b = load_codes(bp + (int64_t)k * 128, quarter);
-        const float sb = g.sb[(int64_t)k * g.col_blocks + n0 / 128];
+        for (int d = 0; d < DEPTH; d++) {
+            if (k0 + d * WAVES >= g.blocks) break;
+            Operand<EXACT> b, a;
+            b.set(bc[d]);
+            a.set(ac[d]);
+            const f32x4_t p = block_product<EXACT>(b, a);
 #pragma unroll
-        for (int i = 0; i < MB; i++) {
-            const f32x4_t p = block_product<std::is_same<OUT, float>::value>(b, load_codes(ap[i] + (int64_t)k * 128, quarter));
-            const float scale = sb * g.sa[(int64_t)k * g.rows + m[i]];
-#pragma unroll
-            for (int j = 0; j < 4; j++) acc[i][j] = fmaf(p[j], scale, acc[i][j]);
+            for (int j = 0; j < 4; j++) acc[j] = fmaf(p[j], scale[d], acc[j]);
         }
     }
-#pragma unroll
-    for (int i = 0; i < MB; i++) part[wave][i][lane] = acc[i];
+    part[wave][lane] = acc;
     __syncthreads();
-    for (int i = wave; i < MB; i += WAVES) {
-        f32x4_t v = part[0][i][lane];
+    if (wave > 0) return;
+    f32x4_t v = part[0][lane];
 #pragma unroll
-        for (int w = 1; w < WAVES; w++) v += part[w][i][lane];
-        if (m0 + 16 * i + row < g.rows) store_out<OUT>(g, m0 + 16 * i + row, n0 + 4 * quarter, v);
+    for (int w = 1; w < WAVES; w++) v += part[w][lane];
+    if (m0 + row < g.rows) store_out<OUT>(g, m0 + row, n0 + 4 * quarter, v);
+}
+
+// 4-byte global -> LDS copy without a register stop: lane l writes LDS bytes [lds_base + 4 * l, +4).
+__device__ inline void copy4_global_to_lds(const void* sbase, uint32_t voff, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1\n" : : "v"(voff), "s"(sbase), "s"(lds_base) : "memory");
+}
+
+// BN columns x BM rows per workgroup of WN x WM wavefronts, each a grid of 16 x 16 blocks.  A stage holds one block of
+// 128 of the reduction: BN rows of b, BM rows of a (128 bytes each), their scales.  Two stages: one is multiplied while the
+// other is on its way.  A row's eight 16-byte pieces are stored permuted by the row's number, so that the rows that an
+// instruction's lanes read side by side lie in different banks; the permutation is made by the lanes' choice of
+// what to fetch.  A wavefront keeps its rows of a in registers for the stage and passes over its columns; a product is
+// scaled and added LAG instructions after its own, while those run.
+// A workgroup barrier that waits for nothing else: __syncthreads() also waits for every LDS read under way.
+__device__ inline void barrier() { asm volatile("s_barrier" : : : "memory"); }
+
+// Rows of a wavefront's MW x NW outputs that its part of LDS takes at a time.
+template <typename OUT>
+constexpr int tile_pass_rows(int NW, int MW)
+{
+    const int most = NW * (int)sizeof(OUT) <= 256 ? 64 : 32;
+    return MW < most ? MW : most;
+}
+
+template <typename OUT, int BN, int BM, int WN, int WM, int KG, bool AHEAD>
+__global__ __launch_bounds__(64 * WN * WM * KG, 2) void k_matmul_tile(MatmulArgs g)
+{
+    constexpr bool EXACT = std::is_same<OUT, float>::value;
+    constexpr int WAVES = WN * WM, FN = BN / WN / 16, FM = BM / WM / 16, LAG = 3;
+    constexpr int STAGE = (BN + BM) * 128 + BM * 4 + 256;      // codes of b, of a; scales of a, of b
+    constexpr int CB = BN * 8 / (64 * WAVES), CA = BM * 8 / (64 * WAVES), COPIES = CB + CA + 1;
+    static_assert(BM / 64 < WAVES && BM % 64 == 0, "a wavefront of its own for b's scales");
+    static_assert((BN / WN) % 16 == 0 && 128 % (BN / WN) == 0, "a wavefront's columns lie in one block of 128");
+    extern __shared__ __align__(16) uint8_t lds[];
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), kg = all / WAVES, wave = all % WAVES;
+    const int wn = wave % WN, wm = wave / WN, row = lane & 15, quarter = lane >> 4;
+
+    // Workgroups go to the 8 XCDs in turn: each gets a run of neighbouring tiles, 8 rows of tiles at a time, so that those
+    // which run together share rows of a and b in its L2
+    const uint32_t tile = (blockIdx.x & 7) * g.per_xcd + (blockIdx.x >> 3);
+    if (tile >= g.tiles) return;
+    const uint32_t strip = tile / (8 * g.col_tiles), in_strip = tile - strip * 8 * g.col_tiles;
+    const uint32_t high = g.row_tiles - 8 * strip < 8 ? g.row_tiles - 8 * strip : 8;
+    const int32_t n0 = (int32_t)(in_strip / high) * BN;
+    const int64_t m0 = (int64_t)(8 * strip + in_strip % high) * BM;
+
+    // what this lane copies of every stage: 16-byte piece `lane % 8`, permuted, of a row of b / of a; one scale.  Rows past
+    // the end repeat the last.
+    uint32_t bo[CB], ao[CA];
+#pragma unroll
+    for (int i = 0; i < CB; i++) {
+        const int32_t r = (i * WAVES + wave) * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+        bo[i] = (uint32_t)(n0 + r < g.cols ? r : g.cols - 1 - n0) * (uint32_t)g.bs + c * 16;
     }
+#pragma unroll
+    for (int i = 0; i < CA; i++) {
+        const int32_t r = (i * WAVES + wave) * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+        ao[i] = (uint32_t)(m0 + r < g.rows ? r : (int32_t)(g.rows - 1 - m0)) * (uint32_t)g.as + c * 16;
+    }
+    const uint8_t *bp = g.b + n0 * g.bs, *ap = g.a + m0 * g.as;
+    const bool of_a = wave < BM / 64;
+    const int32_t sm = wave * 64 + lane, sn = n0 / 128 + lane;
+    const uint32_t so = 4 * (uint32_t)(of_a ? (m0 + sm < g.rows ? sm : (int32_t)(g.rows - 1 - m0)) : (sn < g.col_blocks ? sn : g.col_blocks - 1));
+    const float* sp = of_a ? g.sa + m0 : g.sb;
+    const int64_t sstep = of_a ? g.rows : g.col_blocks;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)lds;
+    const uint32_t scale_at = (BN + BM) * 128 + (of_a ? wave * 256 : BM * 4);
+    const int32_t steps = (g.blocks + KG - 1) / KG, mine_steps = (g.blocks - kg + KG - 1) / KG;
+    auto fetch = [&](int32_t t) {
+        const int64_t k = (int64_t)t * KG + kg;
+        const uint32_t st = lds0 + ((t & 1) * KG + kg) * STAGE;
+#pragma unroll
+        for (int i = 0; i < CB; i++) copy16_global_to_lds(bp + k * 128, bo[i], st + (i * WAVES + wave) * 1024);
+#pragma unroll
+        for (int i = 0; i < CA; i++) copy16_global_to_lds(ap + k * 128, ao[i], st + BN * 128 + (i * WAVES + wave) * 1024);
+        copy4_global_to_lds(sp + k * sstep, so, st + scale_at);
+    };
+
+    f32x4_t acc[FN][FM];
+#pragma unroll
+    for (int i = 0; i < FN; i++)
+#pragma unroll
+        for (int j = 0; j < FM; j++) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+    // row r's 32 codes of this lane's quarter, as load_codes takes them
+    const int p0 = (quarter ^ (row & 7)) * 16, p1 = ((quarter + 4) ^ (row & 7)) * 16;
+    auto operand = [&](const uint8_t* rows16) {
+        const int4 lo = *(const int4*)(rows16 + row * 128 + p0), hi = *(const int4*)(rows16 + row * 128 + p1);
+        return i32x8_t{lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    };
+
+    i32x8_t na[FM], nb;
+    float ns[FM];
+    auto load = [&](int32_t t) {               // a's rows, b's first 16 and the scales of a stage
+        const uint8_t* st = lds + ((t & 1) * KG + kg) * STAGE;
+        const float* sa = (const float*)(st + (BN + BM) * 128);
+        nb = operand(st + wn * (BN / WN) * 128);
+        const float sb = sa[BM + wn * (BN / WN) / 128];
+#pragma unroll
+        for (int j = 0; j < FM; j++) {
+            na[j] = operand(st + (BN + wm * (BM / WM) + j * 16) * 128);
+            ns[j] = sa[wm * (BM / WM) + 16 * j + row] * sb;
+        }
+    };
+
+    Operand<EXACT> a[FM], b;
+    float scale[FM];
+    f32x4_t p[LAG + 1];
+    auto add = [&](int q) {
+        const int i = q / FM, j = q % FM;
+#pragma unroll
+        for (int r = 0; r < 4; r++) acc[i][j][r] = fmaf(p[q % (LAG + 1)][r], scale[j], acc[i][j][r]);
+        asm volatile("" : "+v"(acc[i][j]));      // here: else the compiler sinks it behind the loop's end, and all products stay in registers
+    };
+    auto take = [&]() {
+#pragma unroll
+        for (int j = 0; j < FM; j++) {
+            a[j].set(na[j]);
+            scale[j] = ns[j];
+        }
+    };
+    auto column = [&](int i) {                 // 16 columns' products with all rows
+#pragma unroll
+        for (int j = 0; j < FM; j++) {
+            const int q = i * FM + j;
+            p[q % (LAG + 1)] = block_product<EXACT>(b, a[j]);
+            if (q >= LAG) add(q - LAG);
+        }
+    };
+    auto columns = [&](const uint8_t* bst, int count) {
+#pragma unroll
+        for (int i = 0; i < count; i++) {
+            b.set(nb);
+            if (i + 1 < FN) nb = operand(bst + (i + 1) * 16 * 128);
+            if (AHEAD) __builtin_amdgcn_s_setprio(1);
+            column(i);
+            if (AHEAD) __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    auto finish = [&]() {
+#pragma unroll
+        for (int q = FN * FM - LAG; q < FN * FM; q++) add(q);
+    };
+
+    if (mine_steps > 0) fetch(0);
+    if (mine_steps > 1) fetch(1);
+    if constexpr (AHEAD) {
+        // One workgroup per compute unit: the next stage's first operands are read while this one's last columns are
+        // multiplied, so that no wavefront begins a step by waiting for LDS
+        static_assert(KG == 1, "");
+        if (steps > 1) wait_vmcnt<COPIES>();
+        else wait_vmcnt<0>();
+        barrier();
+        load(0);
+        for (int32_t t = 0; t < steps; t++) {
+            take();
+            columns(lds + (t & 1) * STAGE + wn * (BN / WN) * 128, FN - 1);
+            b.set(nb);
+            wait_vmcnt<0>();
+            barrier();                         // all have read this stage to its end, and the next one has arrived
+            if (t + 1 < steps) load(t + 1);
+            column(FN - 1);
+            finish();
+            if (t + 2 < steps) fetch(t + 2);
+        }
+    } else {
+        for (int32_t t = 0; t < steps; t++) {
+            if (t + 1 < mine_steps) wait_vmcnt<COPIES>();
+            else wait_vmcnt<0>();
+            barrier();
+            if (KG == 1 || t < mine_steps) {
+                load(t);
+                take();
+                columns(lds + ((t & 1) * KG + kg) * STAGE + wn * (BN / WN) * 128, FN);
+                finish();
+            }
+            barrier();
+            if (t + 2 < mine_steps) fetch(t + 2);
+        }
+    }
+
+    if constexpr (KG > 1) {
+        // the groups' sums, added in order by the first
+        f32x4_t* part = (f32x4_t*)lds + (wave * FN * FM) * 64 + lane;
+        constexpr int GROUP = WAVES * FN * FM * 64;
+        if (kg > 0)
+#pragma unroll
+            for (int q = 0; q < FN * FM; q++) part[(kg - 1) * GROUP + q * 64] = acc[q / FM][q % FM];
+        __syncthreads();
+        if (kg > 0) return;
+#pragma unroll
+        for (int q = 0; q < FN * FM; q++)
+#pragma unroll
+            for (int w = 0; w < KG - 1; w++) acc[q / FM][q % FM] += part[w * GROUP + q * 64];
+    }
+
+    // Through LDS, a region per wavefront: a lane holds 4 neighbouring columns of a row, which would leave as 8 bytes here and 8
+    // there; from LDS whole runs of a row leave, 16 bytes a lane.
+    constexpr int NW = BN / WN, PITCH = NW * (int)sizeof(OUT) + 16, RP = tile_pass_rows<OUT>(NW, BM / WM), V = 16 / sizeof(OUT), LPR = NW / V;
+    uint8_t* mine = lds + (KG > 1 ? (KG - 1) * BN * BM * 4 : 0) + wave * (PITCH * RP);
+    const int32_t nw = n0 + wn * NW;
+#pragma unroll
+    for (int pass = 0; pass < FM * 16 / RP; pass++) {
+#pragma unroll
+        for (int i = 0; i < FN; i++) {
+            const int32_t n = nw + 16 * i + 4 * quarter;
+            float bias[4];
+#pragma unroll
+            for (int r = 0; r < 4; r++) bias[r] = g.bias && n + r < g.cols ? g.bias[n + r] : 0.0f;
+#pragma unroll
+            for (int jj = 0; jj < RP / 16; jj++) {
+                const f32x4_t v = acc[i][pass * (RP / 16) + jj];
+                OUT* o = (OUT*)(mine + (16 * jj + row) * PITCH) + 16 * i + 4 * quarter;
+#pragma unroll
+                for (int r = 0; r < 4; r++) o[r] = (OUT)(v[r] + bias[r]);
+            }
+        }
+        const int c = (lane % LPR) * V;
+#pragma unroll
+        for (int r = 0; r < RP; r += 64 / LPR) {
+            const int64_t m = m0 + wm * (BM / WM) + pass * RP + r + lane / LPR;
+            const OUT* from = (const OUT*)(mine + (r + lane / LPR) * PITCH) + c;
+            OUT* o = (OUT*)g.out + m * g.os + nw + c;
+            if (m < g.rows) {
+                if (nw + c + V <= g.cols) {
+                    __builtin_memcpy(o, from, 16);
+                } else {
+#pragma unroll
+                    for (int q = 0; q < V; q++)
+                        if (nw + c + q < g.cols) o[q] = from[q];
+                }
+            }
+        }
+    }
+}
+
+template <typename OUT, int BN, int BM, int WN, int WM, int KG, bool AHEAD>
+static int launch_tile(MatmulArgs g, hipStream_t s)
+{
+    constexpr int stages = 2 * KG * ((BN + BM) * 128 + BM * 4 + 256);
+    constexpr int outputs = (KG - 1) * BN * BM * 4 + WN * WM * (BN / WN * (int)sizeof(OUT) + 16) * tile_pass_rows<OUT>(BN / WN, BM / WM);
+    constexpr int lds = stages > outputs ? stages : outputs;
+    static_assert(lds <= 160 * 1024 && (BM / WM) % tile_pass_rows<OUT>(BN / WN, BM / WM) == 0, "");
+    g.col_tiles = (uint32_t)((g.cols + (int64_t)BN - 1) / BN);
+    g.row_tiles = (uint32_t)((g.rows + (int64_t)BM - 1) / BM);
+    const int64_t n = (int64_t)g.col_tiles * g.row_tiles;
+    if (n > INT32_MAX / 2) return ICV_ERR_INVALID_ARG;
+    g.tiles = (uint32_t)n;
+    g.per_xcd = (uint32_t)((n + 7) / 8);
+    const auto kernel = k_matmul_tile<OUT, BN, BM, WN, WM, KG, AHEAD>;
+    ICV_HIP_CHECK(hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+    kernel<<<8 * g.per_xcd, 64 * WN * WM * KG, lds, s>>>(g);
+    ICV_HIP_CHECK(hipGetLastError());
+    return ICV_OK;
+}
+
+template <typename OUT, int WAVES>
+static int launch_split(const MatmulArgs& g, hipStream_t s)
+{
+    const int64_t n = ((g.cols + (int64_t)15) / 16) * ((g.rows + (int64_t)15) / 16);
+    if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
+    k_matmul_split<OUT, WAVES><<<(uint32_t)n, 64 * WAVES, 0, s>>>(g);
+    ICV_HIP_CHECK(hipGetLastError());
+    return ICV_OK;
+}
+
+// The kernels a product can run on, and what each takes, in us, fitted to 60 products of 1 to 16384 rows, 64 to 16384
+// columns and depth (MI355X, operands not in L2): `alone` for a step (a block of the reduction of every group) where a
+// compute unit has no more than one workgroup, `busy` for each step of each workgroup where it has more, `out` for a tile's
+// outputs.  The fastest by this model took 1.04 times as long as the fastest measured; leaving the 128 x 64 tile out
+// 1.05, the tiles of 32 x 64 whose 4 groups share the reduction 1.12 (64 rows, 8192 columns, 4096 deep: 11.5 us, 15.5 with 64 x 64).
+// Float outputs have no 256 x 256 tile: widened operands leave no room in the registers (5284 x 6015, 256 deep: 49.6 us, 38.3 with
+// 128 x 64).
+struct MatmulKernel {
+    int32_t cols, rows, groups;
+    double alone, busy, out;
+};
+enum { TILE_256 = 0, TILE_128, TILE_128_64, TILE_64, TILE_32_64, SPLIT, KERNELS };
+static const MatmulKernel kKernels[2][KERNELS] = {
+    {{256, 256, 1, 2.5, 2.5, 2.0}, {128, 128, 1, 0.78, 1.05, 0.71}, {128, 64, 1, 0.51, 0.50, 0.42}, {64, 64, 1, 0.35, 0.27, 0.26},
+     {32, 64, 4, 0.64, 1.36, 0.25}, {16, 16, 8, 0.65, 0.61, 0.0}},
+    {{256, 256, 1, 1e9, 1e9, 0.0}, {128, 128, 1, 1.14, 1.80, 1.03}, {128, 64, 1, 0.72, 0.85, 0.54}, {64, 64, 1, 0.48, 0.52, 0.22},
+     {32, 64, 4, 0.93, 1.83, 0.11}, {16, 16, 8, 0.62, 0.67, 0.0}}};
+
+static int choose_kernel(const MatmulArgs& g, bool exact)
+{
+    // the tile kernels keep a tile's offsets in 32 bits
+    if (g.as >= (1 << 23) || g.bs >= (1 << 23)) return SPLIT;
+    int best = SPLIT;
+    double least = 1e30;
+    for (int k = 0; k < KERNELS; k++) {
+        const MatmulKernel& m = kKernels[exact][k];
+        const double tiles = (double)((g.cols + (int64_t)m.cols - 1) / m.cols) * (double)((g.rows + (int64_t)m.rows - 1) / m.rows);
+        const double steps = (double)((g.blocks + m.groups - 1) / m.groups);
+        const double turns = k == TILE_256 ? ceil(tiles / 256) : tiles / 256;      // one workgroup per compute unit, or several
+        const double us = fmax(steps * m.alone, turns * steps * m.busy) + fmax(turns, 1.0) * m.out;
+        if (us < least) { least = us; best = k; }
+    }
+    return best;
 }
 
 template <typename OUT>
 static int launch(const MatmulArgs& g, hipStream_t s)
 {
-    constexpr int MB = 4, WAVES = 4;
-    const int64_t n = (int64_t)((g.cols + 15) / 16) * (((int64_t)g.rows + 16 * MB - 1) / (16 * MB));
-    if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-    k_matmul_split<OUT, MB, WAVES><<<(uint32_t)n, 64 * WAVES, 0, s>>>(g);
-    ICV_HIP_CHECK(hipGetLastError());
-    return ICV_OK;
+    constexpr bool EXACT = std::is_same<OUT, float>::value;
+    switch (choose_kernel(g, EXACT)) {
+        case TILE_256:
+            if constexpr (!EXACT) return launch_tile<OUT, 256, 256, 2, 4, 1, true>(g, s);
+        case TILE_128: return launch_tile<OUT, 128, 128, 2, 2, 1, false>(g, s);
+        case TILE_128_64: return launch_tile<OUT, 128, 64, 2, 2, 1, false>(g, s);
+        case TILE_64: return launch_tile<OUT, 64, 64, 2, 2, 1, false>(g, s);
+        case TILE_32_64: return launch_tile<OUT, 32, 64, 1, 2, 4, false>(g, s);
+        default:
+            // wavefronts without a block would only make the sums' exchange longer: 1 x 1024, 64 deep 5.4 us with 8, 4.3 with 4
+            return g.blocks <= 4 ? launch_split<OUT, 4>(g, s) : launch_split<OUT, 8>(g, s);
+    }
 }
 
 }  // namespace icv

@@ -121,6 +121,19 @@ def test_matmul_larger(M, N, K):
     matmul_case(M, N, K, "bf16", False, M + K)
 
 
+@pytest.mark.parametrize("M,N,K,out", [
+    # every kernel on sizes that are no multiple of its tile, the reduction of one block, of an odd number and of many
+    (3000, 5000, 128, "bf16"), (2900, 3100, 1100, "bf16"), (2177, 4100, 2400, "bf16"),     # 256 x 256
+    (1500, 3100, 900, "bf16"), (2900, 3100, 1100, "f32"), (3000, 4100, 129, "f32"),        # 128 x 128
+    (1100, 2050, 700, "bf16"), (1100, 2050, 700, "f32"),                                   # 128 x 64
+    (500, 2050, 384, "bf16"), (700, 1030, 600, "f32"),                                     # 64 x 64
+    (100, 2050, 3000, "bf16"), (70, 1030, 2200, "f32"), (64, 100, 500, "bf16"),            # 32 x 64 in four groups
+    (13, 1000, 8000, "bf16"), (3, 500, 512, "f32"), (1, 4099, 1920, "f32"),                # 16 x 16 in eight or four
+])
+def test_matmul_every_tile(M, N, K, out):
+    matmul_case(M, N, K, out, True, M + N + K, pad=M % 2)
+
+
 def test_matmul_scales_of_very_different_size():
     matmul_case(70, 300, 1024, "f32", True, 5, far=True)
     matmul_case(600, 520, 1024, "f32", False, 6, far=True)
