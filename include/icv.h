@@ -325,7 +325,7 @@ ICV_API int icv_causal_conv1d(const icv_causal_conv_params* p, const icv_sequenc
  */
 typedef struct icv_scan_params {
     int32_t channels, states, groups;   /* states 1..64 (more: ICV_ERR_UNSUPPORTED); groups divides channels */
-    int32_t x_row_stride, dt_row_stride, b_row_stride, c_row_stride, z_row_stride, out_row_stride;
+    int32_t x_row_stride, dt_row_stride, b_row_stride, c_row_stride, z_row_stride, out_row_stride;  /* 2^24 and more: ICV_ERR_UNSUPPORTED */
     int32_t dtype;                      /* ICV_F32 or ICV_BF16: x, dt, B, C, z, out */
     int32_t softplus;                   /* 0 or 1 */
     int32_t state_slots;

@@ -1,8 +1,10 @@
 // Selective state space scan (icv_selective_scan).
 //
-// Per row, channel and state: one exponential (the decay), two products and two multiply-adds.  Vector-ALU bound: about
-// 24 issue cycles for 64 of them (8 for the exponential, 4 for each of the others), against 2 to 8 bytes of memory
-// per row and channel.
+// Per row, channel and state: one exponential (the decay), two products and two multiply-adds.  Vector-ALU bound: 24 issue
+// cycles for 64 of them (8 for the exponential, 4 for each of the others), and about 40 instructions per row and channel around
+// them (softplus, gate, conversions), against 2 to 8 bytes of memory per row and channel.  24 sequences of 12347 rows, 4096
+// channels, 16 states, bfloat16 with gate: 290 us, of which the instructions alone take 250 (525 us at first: what was in the way
+// were waits for the next tile's loads inside conversions and branches, 64-bit address products, and bank conflicts).
 //
 // A lane keeps 4 states of a channel in registers, S lanes (1..16) a channel: the rows' delta and delta * x are then read
 // from LDS once for 4 states, and a channel's states take few enough registers for several workgroups on a compute
@@ -22,6 +24,7 @@ struct ScanArgs {
     void* out;
     int64_t xs, dts, bs, cs, zs, os, slot_stride;
     int32_t channels, states, per_group, group_tiles, softplus;
+    int32_t by_length;        // longest sequences first
     int32_t chunk, units;     // rows per piece of a sequence (0: sequences are not cut), pieces there is room for
     float *ws_state, *ws_sum; // of every piece: [channels][states] and [channels]
     SeqArgs seq;
@@ -31,25 +34,41 @@ enum { SCAN_WHOLE = 0, SCAN_PIECE_STATE = 1, SCAN_PIECE_OUT = 2 };
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
-// log(1 + exp(v)).  With e = exp(v) and u = 1 + e rounded, log(1 + e) = log(u) + log(1 + (e - (u - 1)) / u), the second
-// term being a rounding error small enough for its first order: exact to a few ulp for every v, tiny e included.
+// log(1 + exp(v)) = max(v, 0) + log(1 + e), e = exp(-|v|).  With u = 1 + e rounded, log(1 + e) = log(u) + log(1 + (e - (u - 1)) / u): the
+// second term is the rounding error of u, at most 2^-24, and what counts of it is there where e is small and u is 1, so
+// that the quotient may be left out: exact to a few ulp for every v.
 __device__ inline float softplus(float v)
 {
-    const float e = __builtin_amdgcn_exp2f(v * kLog2e), u = 1.0f + e;
-    const float s = fmaf(__builtin_amdgcn_logf(u), kLn2, (e - (u - 1.0f)) * __builtin_amdgcn_rcpf(u));
-    return v > 20.0f ? v : s;         // exp(-20) is below half an ulp of 20
+    const float e = __builtin_amdgcn_exp2f(fabsf(v) * -kLog2e), u = 1.0f + e;
+    return fmaxf(v, 0.0f) + fmaf(__builtin_amdgcn_logf(u), kLn2, e - (u - 1.0f));
 }
 
-template <int N, typename T>
-__device__ inline void load_raw(const T* p, int n, T (&r)[N])
-{
-    if (n >= N) {
-        __builtin_memcpy(r, p, sizeof(r));
-    } else {
-#pragma unroll
-        for (int j = 0; j < N; j++) r[j] = j < n ? p[j] : (T)0.0f;
+// N neighbouring elements on their way to registers, held as loaded: taken apart where they are loaded, they would be waited
+// for there.  ODD: some may not be there (an odd group of channels, a number of states that is no multiple of 4), so each
+// is loaded by itself, from the last one that is there if need be.
+template <typename T, int N, bool ODD>
+struct Raw {
+    uint32_t w[ODD ? N : N * sizeof(T) / 4];
+    __device__ float get(int j) const
+    {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[j]);
+        else if constexpr (ODD) return __builtin_bit_cast(float, w[j] << 16);
+        else return __builtin_bit_cast(float, j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
     }
-}
+    __device__ void load(const uint8_t* base, uint32_t at, int n)       // n of them are there, or none
+    {
+        if constexpr (!ODD) {
+            __builtin_memcpy(w, base + at, sizeof(w));
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; j++) {
+                const uint8_t* p = base + at + (j < n ? j : 0) * sizeof(T);
+                if constexpr (sizeof(T) == 4) w[j] = *(const uint32_t*)p;
+                else w[j] = *(const uint16_t*)p;
+            }
+        }
+    }
+};
 
 // lane -> its place among the S lanes of a channel, and the channel among the wavefront's.  The four lowest states of a
 // channel sit in one quad; with 8 lanes the second quad is 8 lanes away, with 16 all of a row of 16 is one channel's,
@@ -96,12 +115,36 @@ __device__ inline void load_states(const float* p, int nv, float (&h)[4])
     load_row<4>(p, nv, h);
 }
 
-template <typename T, int S, bool PAD, int MODE>
+// The n-th of at most 64 sequences by length, longest first; the same for all lanes.  Workgroups start in the order of their
+// numbers, and a long sequence that starts last keeps a few compute units busy alone: 24 sequences of 12347 rows and 4096 channels
+// took 412 us as they came, 376 by length.
+__device__ inline int32_t nth_longest(const SeqArgs& q, int32_t n, int lane)
+{
+    int32_t length = -1;
+    if (lane < q.count) {
+        const int32_t b = seq_begin(q, lane);
+        length = seq_end(q, lane, b) - b;
+    }
+    int32_t rank = 0;
+    for (int k = 0; k < q.count; k++) {
+        const int32_t other = __builtin_amdgcn_readlane(length, k);
+        rank += other > length || (other == length && k < lane);
+    }
+    return __builtin_ctzll(__ballot(lane < q.count && rank == n));
+}
+
+// Two rows' values of a lane's channel and states.
+struct Rows2 {
+    float2 v[2];
+    float4 b[2], c[2];
+};
+
+template <typename T, int S, bool ODD, int MODE>
 __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
 {
-    constexpr int CW = 256 / S, TT = 8 * S < 64 ? 8 * S : 64, PPT = TT * CW / 256, VPR = CW / PPT;
+    constexpr int CW = 256 / S, TT = 8 * S < 64 ? 8 * S : 64, PAIRS = CW / 2, RPT = TT * PAIRS / 256, ROWS = TT / RPT;
     constexpr int BCV = (TT * S + 255) / 256;      // vectors of 4 states of B (and C) a thread stages
-    __shared__ float2 dtx[TT][CW];                  // delta and delta * x; the row's output takes delta's place
+    __shared__ __align__(16) float2 dtx[TT][CW];    // delta and delta * x; the row's output takes delta's place
     __shared__ float4 sB[TT][S], sC[MODE == SCAN_PIECE_STATE ? 1 : TT][S];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -110,6 +153,7 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
     int32_t unit = (int32_t)(blockIdx.x / tiles), piece = 0, pieces = 1, i = unit;
     int32_t begin, end;
     if (MODE == SCAN_WHOLE) {
+        if (a.by_length) i = nth_longest(a.seq, unit, lane);
         begin = seq_begin(a.seq, i);
         end = seq_end(a.seq, i, begin);
         if (begin == end) return;
@@ -161,94 +205,151 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
         if (MODE == SCAN_PIECE_STATE && ch < cn) store_row<4>(a.ws_state + (first_unit + pieces - 1) * plane + state_at, nv, h);
     } else if (MODE == SCAN_PIECE_OUT) {
         load_states(a.ws_state + (piece == 0 ? first_unit + pieces - 1 : first_unit) * plane + state_at, nv, h);
-        for (int32_t q = 1; q < piece; q++) {
-            const float sum = a.ws_sum[(int64_t)(first_unit + q) * a.channels + d];
-            float w[4];
-            load_states(a.ws_state + (first_unit + q) * plane + state_at, nv, w);
+        for (int32_t q0 = 1; q0 < piece; q0 += 8) {
+            float sum[8], w[8][4];
 #pragma unroll
-            for (int j = 0; j < 4; j++) h[j] = fmaf(__builtin_amdgcn_exp2f(sum * A[j]), h[j], w[j]);
+            for (int u = 0; u < 8; u++) {              // past the last: the first again, not used
+                const int32_t q = first_unit + (q0 + u < piece ? q0 + u : q0);
+                sum[u] = a.ws_sum[(int64_t)q * a.channels + d];
+                load_states(a.ws_state + q * plane + state_at, nv, w[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < 8; u++)
+                if (q0 + u < piece)
+#pragma unroll
+                    for (int j = 0; j < 4; j++) h[j] = fmaf(__builtin_amdgcn_exp2f(sum[u] * A[j]), h[j], w[u][j]);
         }
     }
 
-    // staging: thread -> row and PPT channels of the tile, and vectors of B and C
-    const int vrow = tid / VPR, vch = (tid % VPR) * PPT;
-    const int vn = cn - vch < 0 ? 0 : (cn - vch < PPT ? cn - vch : PPT);
-    float dtb[PPT], Dx[PPT];
+    // staging: a thread takes two neighbouring channels of RPT of the tile's rows (lanes side by side read a row's channels
+    // side by side, and meet no bank conflicts in LDS), and vectors of B and C
+    const int vrow = tid / PAIRS, vch = 2 * (tid % PAIRS);
+    const int vn = cn - vch < 0 ? 0 : (cn - vch < 2 ? cn - vch : 2);
+    float dtb[2], Dx[2];
 #pragma unroll
-    for (int j = 0; j < PPT; j++) {
+    for (int j = 0; j < 2; j++) {
         dtb[j] = a.dtb && j < vn ? a.dtb[c0 + vch + j] : 0.0f;
         Dx[j] = a.D && j < vn ? a.D[c0 + vch + j] : 0.0f;
     }
-    const T* xp = (const T*)a.x + c0 + vch;
-    const T* dtp = (const T*)a.dt + c0 + vch;
-    const T* zp = (const T*)a.z + c0 + vch;
-    T* op = (T*)a.out + c0 + vch;
-    T nx[PPT], nd[PPT], nz[PPT], nB[BCV][4], nC[BCV][4];
-    auto fetch = [&](int32_t r) {
-        const int n = r + vrow < row1 ? vn : 0;
-        const int64_t t = n ? r + vrow : row0;
-        load_raw<PPT>(xp + t * a.xs, n, nx);
-        load_raw<PPT>(dtp + t * a.dts, n, nd);
-        if (MODE != SCAN_PIECE_STATE && a.z) load_raw<PPT>(zp + t * a.zs, n, nz);
+    // Offsets inside a tile are 32-bit and the same for every tile, what moves is a scalar base: with 64-bit products for every
+    // row a third of all vector instructions were address arithmetic.
+    constexpr uint32_t SZ = sizeof(T);
+    const uint32_t vc = c0 + (vn ? vch : 0);
+    const uint32_t xo = (vrow * (uint32_t)a.xs + vc) * SZ, dto = (vrow * (uint32_t)a.dts + vc) * SZ, zo = (vrow * (uint32_t)a.zs + vc) * SZ,
+                   oo = vrow * (uint32_t)a.os + vc;
+    const auto row_of = [](const void* p, int64_t row, int64_t stride) { return (const uint8_t*)p + row * stride * SZ; };      // scalar
+    // Rows past the end repeat the last one (and are made to change nothing when they are staged): loads without branches
+    constexpr int BCT = TT * S < 256 ? TT * S : 256;               // threads with B and C of their own; the others repeat them
+    const int bct = tid % BCT, n4 = 4 * (bct % S), bcrow = bct / S;
+    const int bcn = a.states - n4 < 0 ? 0 : (a.states - n4 < 4 ? a.states - n4 : 4);
+    const uint32_t bc0 = (uint32_t)group * a.states + (bcn ? n4 : 0);
+    Raw<T, 2, ODD> nx[RPT], nd[RPT], nz[RPT];
+    Raw<T, 4, ODD> nB[BCV], nC[BCV];
+    auto fetch_tile = [&](int32_t r, auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        const int32_t most = row1 - 1 - r;
+        const auto pairs = [&](Raw<T, 2, ODD> (&q)[RPT], const void* p, int64_t stride, uint32_t at) {
 #pragma unroll
-        for (int q = 0; q < BCV; q++) {
-            const int v = tid + 256 * q, row = v / S, n4 = 4 * (v % S);
-            if (TT * S % 256 != 0 && row >= TT) continue;
-            int m = a.states - n4 < 0 ? 0 : (a.states - n4 < 4 ? a.states - n4 : 4);
-            if (r + row >= row1) m = 0;
-            const int64_t tb = m ? r + row : row0;
-            load_raw<4>((const T*)a.B + tb * a.bs + (int64_t)group * a.states + (m ? n4 : 0), m, nB[q]);
-            if (MODE != SCAN_PIECE_STATE)
-                load_raw<4>((const T*)a.C + tb * a.cs + (int64_t)group * a.states + (m ? n4 : 0), m, nC[q]);
-        }
+            for (int k = 0; k < RPT; k++) {
+                if constexpr (WHOLE) {
+                    q[k].load(row_of(p, r + k * ROWS, stride), at, vn);
+                } else {
+                    const int32_t row = vrow + k * ROWS;
+                    q[k].load(row_of(p, r, stride), ((uint32_t)(row < most ? row : most) * (uint32_t)stride + vc) * SZ, vn);
+                }
+            }
+        };
+        pairs(nx, a.x, a.xs, xo);
+        pairs(nd, a.dt, a.dts, dto);
+        if (MODE != SCAN_PIECE_STATE && a.z) pairs(nz, a.z, a.zs, zo);
+        const auto fours = [&](Raw<T, 4, ODD> (&q)[BCV], const void* p, int64_t stride) {
+            const uint8_t* base = row_of(p, r, stride);
+#pragma unroll
+            for (int k = 0; k < BCV; k++) {
+                int32_t row = bcrow + k * (256 / S);
+                if (!WHOLE && row > most) row = most;
+                q[k].load(base, ((uint32_t)row * (uint32_t)stride + bc0) * SZ, bcn);
+            }
+        };
+        fours(nB, a.B, a.bs);
+        if (MODE != SCAN_PIECE_STATE) fours(nC, a.C, a.cs);
+    };
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    auto fetch = [&](int32_t r) {
+        if (r + TT <= row1) fetch_tile(r, yes);
+        else fetch_tile(r, no);
     };
 
     float total = 0.0f;                       // sum of delta over the piece
     fetch(row0);
     for (int32_t r = row0; r < row1; r += TT) {
-        const int n = r + vrow < row1 ? vn : 0;
-        T cx[PPT], cz[PPT];
+        Raw<T, 2, ODD> cx[RPT], cz[RPT];
+        const bool tail = r + TT > row1;
 #pragma unroll
-        for (int j = 0; j < PPT; j++) {
-            cx[j] = nx[j]; cz[j] = nz[j];
-            float v = (float)nd[j] + dtb[j];
-            if (a.softplus) v = softplus(v);
-            if (j >= n) v = 0.0f;             // rows past the end and channels past the tile: decay 1, nothing added
-            dtx[vrow][vch + j] = make_float2(v, j < n ? v * (float)nx[j] : 0.0f);
+        for (int k = 0; k < RPT; k++) {
+            cx[k] = nx[k];
+            cz[k] = nz[k];
+            float v[2] = {nd[k].get(0) + dtb[0], nd[k].get(1) + dtb[1]};
+            if (a.softplus) { v[0] = softplus(v[0]); v[1] = softplus(v[1]); }
+            float4 q = make_float4(v[0], v[0] * cx[k].get(0), v[1], v[1] * cx[k].get(1));
+            if (tail && r + vrow + k * ROWS >= row1) q = make_float4(0.0f, 0.0f, 0.0f, 0.0f);      // decay 1, nothing added
+            *(float4*)&dtx[vrow + k * ROWS][vch] = q;
         }
 #pragma unroll
-        for (int q = 0; q < BCV; q++) {
-            const int v = tid + 256 * q, row = v / S, sv = v % S;
-            if (TT * S % 256 != 0 && row >= TT) continue;
-            sB[row][sv] = make_float4((float)nB[q][0], (float)nB[q][1], (float)nB[q][2], (float)nB[q][3]);
-            if (MODE != SCAN_PIECE_STATE)
-                sC[row][sv] = make_float4((float)nC[q][0], (float)nC[q][1], (float)nC[q][2], (float)nC[q][3]);
+        for (int k = 0; k < BCV; k++) {
+            const int row = bcrow + k * (256 / S);
+            const bool out = tail && r + row >= row1;
+            const auto values = [&](const Raw<T, 4, ODD>& q) {
+                float4 v = make_float4(q.get(0), q.get(1), q.get(2), q.get(3));
+                if (ODD) v = make_float4(bcn > 0 ? v.x : 0.0f, bcn > 1 ? v.y : 0.0f, bcn > 2 ? v.z : 0.0f, bcn > 3 ? v.w : 0.0f);
+                return out ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : v;
+            };
+            sB[row][n4 / 4] = values(nB[k]);
+            if (MODE != SCAN_PIECE_STATE) sC[row][n4 / 4] = values(nC[k]);
         }
         __syncthreads();
         if (r + TT < row1) fetch(r + TT);
 
+        // four rows at a time, the next two always on their way from LDS; rows past the end change nothing
         const int rows = row1 - r < TT ? row1 - r : TT;
-        for (int t = 0; t < rows; t += 4) {
-            float p[4];
+        Rows2 even, odd;
+        auto read = [&](Rows2& q, int t) {
 #pragma unroll
-            for (int u = 0; u < 4; u++) {
-                const float2 v = dtx[t + u][ch];
-                const float4 b = sB[t + u][s];
-                const float bb[4] = {b.x, b.y, b.z, b.w};
-                p[u] = 0.0f;
+            for (int u = 0; u < 2; u++) {
+                q.v[u] = dtx[t + u][ch];
+                q.b[u] = sB[t + u][s];
+                if (MODE != SCAN_PIECE_STATE) q.c[u] = sC[t + u][s];
+            }
+        };
+        float p[4];
+        auto step = [&](const Rows2& q, int at) {
+#pragma unroll
+            for (int u = 0; u < 2; u++) {
+                const float2 v = q.v[u];
+                const float bb[4] = {q.b[u].x, q.b[u].y, q.b[u].z, q.b[u].w};
                 if (MODE == SCAN_PIECE_STATE) total += v.x;
 #pragma unroll
                 for (int j = 0; j < 4; j++) {
                     h[j] = fmaf(__builtin_amdgcn_exp2f(v.x * A[j]), h[j], v.y * bb[j]);
-                    if (PAD) h[j] = j < nv ? h[j] : 0.0f;    // an infinite input must not reach a state that is not there
+                    if (ODD) h[j] = j < nv ? h[j] : 0.0f;    // an infinite input must not reach a state that is not there
                 }
                 if (MODE != SCAN_PIECE_STATE) {
-                    const float4 c = sC[t + u][s];
-                    const float cc[4] = {c.x, c.y, c.z, c.w};
+                    const float cc[4] = {q.c[u].x, q.c[u].y, q.c[u].z, q.c[u].w};
+                    p[at + u] = cc[0] * h[0];
 #pragma unroll
-                    for (int j = 0; j < 4; j++) p[u] = fmaf(cc[j], h[j], p[u]);
+                    for (int j = 1; j < 4; j++) p[at + u] = fmaf(cc[j], h[j], p[at + u]);
                 }
             }
+        };
+        read(even, 0);
+        for (int t = 0; t < rows; t += 4) {
+            read(odd, t + 2);
+            __builtin_amdgcn_sched_barrier(0);
+            step(even, 0);
+            read(even, t + 4 < TT ? t + 4 : 0);
+            __builtin_amdgcn_sched_barrier(0);
+            step(odd, 2);
             if (MODE != SCAN_PIECE_STATE) {
                 float y[4];
                 reduce_rows<S>(p, s, y);
@@ -264,15 +365,26 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
             }
         }
         __syncthreads();
-        if (MODE != SCAN_PIECE_STATE && n > 0) {
-            float y[PPT];
+        auto store_tile = [&](auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
 #pragma unroll
-            for (int j = 0; j < PPT; j++) {
-                y[j] = dtx[vrow][vch + j].x;
-                if (a.D) y[j] = fmaf(Dx[j], (float)cx[j], y[j]);
-                if (a.z) y[j] *= silu((float)cz[j]);
+            for (int k = 0; k < RPT; k++) {
+                const float4 v = *(const float4*)&dtx[vrow + k * ROWS][vch];
+                float y[2] = {v.x, v.z};
+                if (a.D) {
+                    y[0] = fmaf(Dx[0], cx[k].get(0), y[0]);
+                    y[1] = fmaf(Dx[1], cx[k].get(1), y[1]);
+                }
+                if (a.z) {
+                    y[0] *= silu(cz[k].get(0));
+                    y[1] *= silu(cz[k].get(1));
+                }
+                if (WHOLE || r + vrow + k * ROWS < row1) store_row<2>((T*)a.out + (int64_t)(r + k * ROWS) * a.os + oo, !ODD && WHOLE ? 2 : vn, y);
             }
-            store_row<PPT>(op + (int64_t)(r + vrow) * a.os, n, y);
+        };
+        if (MODE != SCAN_PIECE_STATE) {
+            if (r + TT <= row1 && cn == CW) store_tile(yes);
+            else store_tile(no);
         }
         // the places a thread reads here are the ones it writes for the next tile, and B and C are done with
     }
@@ -286,7 +398,8 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
     }
 }
 
-// One row per sequence: the state is read and written once, which is what bounds it.
+// One row per sequence: the state is read and written once, which is what bounds it (128 sequences, 4096 channels, 16 states, bfloat16:
+// 18.5 us, 3.8 TB/s; two or four sequences per workgroup, their states on their way together, 19.8 and 21.1).
 template <typename T, int S>
 __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
 {
@@ -339,17 +452,23 @@ static int lanes_per_channel(int states)
 
 static bool is_step(const icv_sequences* seq) { return !seq->start && seq->tokens == seq->count; }
 
-// Rows per piece of a sequence, 0 where sequences stay whole.
+// Rows per piece of a sequence, 0 where sequences stay whole.  Pieces cost a second pass over the rows that makes no outputs
+// (0.7 of the first), and fill a chip that whole sequences leave idle: 16384 rows of 2048 channels (32 workgroups) take 1724 us
+// whole, 255 in pieces of 256; 5 sequences of 2501 rows, 1000 channels, 64 states (320 workgroups) 105 whole, waiting for the longest, 77
+// in pieces; 24 of 12347 rows, 4096 channels (1536 workgroups) 290 whole, 400 in pieces.  Equal lengths wait for no one and stay whole
+// from 200 workgroups on (8 x 2048 rows, 256 workgroups: 222 both ways; 6 x 2048: 218 whole, 172 in pieces).  Pieces of less than 128 rows
+// cost more in launches than they save (200 rows, 128 workgroups: 28 whole, 41).
 static int32_t piece_rows(const icv_scan_params* p, const icv_sequences* seq, int S)
 {
     if (is_step(seq)) return 0;
     const int cw = 256 / S, tt = 8 * S < 64 ? 8 * S : 64, per_group = p->channels / p->groups;
     const int64_t wgs = (int64_t)p->groups * ((per_group + cw - 1) / cw) * seq->count;
+    const bool equal = seq->count == 1 || (!seq->start && !seq->length);
     const int64_t mean = seq->tokens / seq->count;
-    if (wgs >= 256 || mean < 512) return 0;
-    const int64_t pieces = (512 + wgs - 1) / wgs;
+    if (wgs >= (equal ? 200 : 512) || mean < (equal ? 320 : 128) || seq->tokens < 320) return 0;
+    const int64_t pieces = (2048 + wgs - 1) / wgs;
     int64_t rows = (mean + pieces - 1) / pieces;
-    if (rows < 256) rows = 256;
+    if (rows < 128) rows = 128;
     return (int32_t)((rows + tt - 1) / tt * tt);
 }
 
@@ -359,7 +478,7 @@ template <typename T, int S>
 static int launch(const ScanArgs& a, bool step, int64_t pieces, hipStream_t s)
 {
     constexpr int CW = 256 / S;
-    const bool pad = a.states != 4 * S;
+    const bool odd = a.states != 4 * S || a.per_group % 2 != 0;
     if (step) {
         const int64_t n = (int64_t)((a.channels + CW - 1) / CW) * a.seq.count;
         if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
@@ -370,15 +489,15 @@ static int launch(const ScanArgs& a, bool step, int64_t pieces, hipStream_t s)
     const int64_t n = (int64_t)a.group_tiles * (a.channels / a.per_group) * (a.chunk ? pieces : a.seq.count);
     if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
     if (!a.chunk) {
-        if (pad) k_scan<T, S, true, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
+        if (odd) k_scan<T, S, true, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
         else k_scan<T, S, false, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
         ICV_HIP_CHECK(hipGetLastError());
         return ICV_OK;
     }
-    if (pad) k_scan<T, S, true, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
+    if (odd) k_scan<T, S, true, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
     else k_scan<T, S, false, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
     ICV_HIP_CHECK(hipGetLastError());
-    if (pad) k_scan<T, S, true, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
+    if (odd) k_scan<T, S, true, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
     else k_scan<T, S, false, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;
@@ -396,6 +515,9 @@ static int launch_lanes(const ScanArgs& a, int S, bool step, int64_t pieces, hip
     }
 }
 
+// A tile's offsets (64 rows at most) are kept in 32 bits.
+constexpr int32_t kMostStride = 1 << 24;
+
 static int check_scan(const icv_scan_params* p, const icv_sequences* seq, SeqArgs* sa)
 {
     if (!p || p->channels < 1 || p->states < 1 || p->groups < 1 || p->channels % p->groups != 0) return ICV_ERR_INVALID_ARG;
@@ -405,6 +527,9 @@ static int check_scan(const icv_scan_params* p, const icv_sequences* seq, SeqArg
     if (p->dtype != ICV_F32 && p->dtype != ICV_BF16) return ICV_ERR_INVALID_ARG;
     for (int32_t r : {p->x_row_stride, p->dt_row_stride, p->z_row_stride, p->out_row_stride})
         if (r && r < p->channels) return ICV_ERR_INVALID_ARG;
+    for (int32_t r : {p->x_row_stride, p->dt_row_stride, p->z_row_stride, p->out_row_stride, p->b_row_stride, p->c_row_stride})
+        if (r >= kMostStride) return ICV_ERR_UNSUPPORTED;
+    if (p->channels >= kMostStride || (int64_t)p->groups * p->states >= kMostStride) return ICV_ERR_UNSUPPORTED;
     for (int32_t r : {p->b_row_stride, p->c_row_stride})
         if (r && r < (int64_t)p->groups * p->states) return ICV_ERR_INVALID_ARG;
     if (p->state_slots < 0 || (p->state_slot_stride && p->state_slot_stride < (int64_t)p->channels * p->states))
@@ -456,6 +581,7 @@ extern "C" int icv_selective_scan(const icv_scan_params* p, const icv_sequences*
     a.channels = p->channels; a.states = p->states; a.per_group = p->channels / p->groups; a.softplus = p->softplus;
     const int S = lanes_per_channel(p->states), cw = 256 / S;
     a.group_tiles = (a.per_group + cw - 1) / cw;
+    a.by_length = (seq->start || seq->length) && seq->count > 1 && seq->count <= 64;
     a.chunk = piece_rows(p, seq, S);
     const int64_t pieces = a.chunk ? piece_count(seq, a.chunk) : 0;
     if (a.chunk && (!workspace || misaligned(workspace, 16))) return ICV_ERR_INVALID_ARG;

@@ -109,6 +109,8 @@ def test_scan_pointers_are_checked(lib):
     assert scan(lib, pointers={"x": at, "out": at}, x_row_stride=32) == BAD            # over x at another stride
     assert scan(lib, pointers={"B": at * 4, "out": at * 4}) == BAD
     assert scan(lib, states=65) == UNSUPPORTED and scan(lib, dtype=icv.ICV_U8I8) == UNSUPPORTED
+    for name in ("x", "dt", "b", "c", "z", "out"):
+        assert scan(lib, **{name + "_row_stride": 1 << 24}) == UNSUPPORTED
     p = icv.make_scan_params(16, 16)
     assert lib.icv_selective_scan(p, seq(), None, None, None) == BAD
     assert lib.icv_selective_scan(None, seq(), icv.icv_scan_tensors(), None, None) == BAD
