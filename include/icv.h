@@ -274,7 +274,7 @@ ICV_API int icv_conv2d_nhwc_im2col_static(const icv_conv_params* p, const void* 
  * undefined.  A slot may be continued by several sequences; a slot that a sequence writes must not be read or written
  * by another one of the same call (reading and writing the same slot by one sequence is the usual case).
  * One new token per sequence is tokens == count without `start`.
- * count = 0 or tokens = 0: nothing to do, ICV_OK.
+ * count = 0 or tokens = 0: nothing to do, ICV_OK.  tokens > 2^31 - 2^16: ICV_ERR_UNSUPPORTED.
  */
 typedef struct icv_sequences {
     int32_t count;

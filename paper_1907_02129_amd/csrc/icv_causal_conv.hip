@@ -1,9 +1,13 @@
 // Short causal convolution along sequences (icv_causal_conv1d).
 //
-// Memory bound: 2 * taps operations per element read and written.  A thread owns VEC neighbouring channels (16 bytes of a
+// Memory bound: 2 * taps operations per element read and written.  A thread owns VEC neighbouring channels (8 bytes of a
 // row) over a run of consecutive rows, keeps the last taps - 1 rows in registers as floats, and so reads every row
-// once, plus taps - 1 rows in front of its run.  Runs are counted over all rows of the call, whatever sequences they
-// belong to, so that ragged batches load the chip evenly; a thread walks the sequences that its run meets.
+// once, plus taps - 1 rows in front of its run; AHEAD rows are on their way at once.  Runs are counted over all rows of the call,
+// whatever sequences they belong to, so that ragged batches load the chip evenly; a thread walks the sequences that its run meets.
+//
+// 24 sequences, 12347 rows, 4096 channels, 4 taps, bfloat16: 50 us, 4.0 TB/s (a copy: 39 us, 5.2 TB/s); 24576 rows, 2048 channels, 2 taps,
+// float: 79 us, 5.1 TB/s.  Registers decide, not the width of a load: with 16 bytes a thread 68 and 90 us, with 4 bytes 51 and 77;
+// 8 rows ahead 52 and 81.
 //
 // The state may be read and written in the same slot, so one thread does both: the run that holds a sequence's first
 // row computes the sequence's first taps - 1 rows (all rows that the old state reaches), also where they pass the run's
@@ -19,15 +23,18 @@ struct ConvArgs {
     void* state;
     void* out;
     int32_t channels, vecs, run, silu;
+    int32_t per_xcd;
     int64_t in_stride, out_stride, slot_stride;
     SeqArgs seq;
 };
 
-template <typename T, int W, int VEC>
+template <typename T, int W, int VEC, int AHEAD>
 __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
 {
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int32_t runs = (a.seq.tokens + a.run - 1) / a.run;
+    using Row = RawRow<T, VEC>;
+    // workgroups go to the 8 XCDs in turn: each gets neighbouring runs, so that the rows in front of a run are in its L2
+    const int64_t id = ((int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3)) * 256 + threadIdx.x;
+    const int32_t runs = (a.seq.tokens - 1) / a.run + 1;
     const int64_t r = id / a.vecs;
     if (r >= runs) return;
     const int32_t c0 = (int32_t)(id - r * a.vecs) * VEC;
@@ -38,12 +45,22 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
     const int32_t r0 = (int32_t)r * a.run, r1 = a.seq.tokens - r0 < a.run ? a.seq.tokens : r0 + a.run;
 
     float w[W][VEC], bias[VEC];
+    {
+        // the filter's rows of these channels lie side by side
+        const T* f = (const T*)a.filt + (int64_t)c0 * W;
+        T q[VEC * W];
+        if (nv == VEC) {
+            __builtin_memcpy(q, f, sizeof(q));
+        } else {
 #pragma unroll
-    for (int j = 0; j < VEC; j++) {
-        const int32_t c = c0 + (j < nv ? j : 0);
-        bias[j] = a.bias ? a.bias[c] : 0.0f;
+            for (int j = 0; j < VEC * W; j++) q[j] = j < nv * W ? f[j] : (T)0.0f;
+        }
 #pragma unroll
-        for (int k = 0; k < W; k++) w[k][j] = (float)((const T*)a.filt)[(int64_t)c * W + k];
+        for (int j = 0; j < VEC; j++) {
+            bias[j] = a.bias && j < nv ? a.bias[c0 + j] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < W; k++) w[k][j] = (float)q[j * W + k];
+        }
     }
 
     // the last sequence that begins at or before the run's first row, else the first one
@@ -70,40 +87,50 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
         if (owner && hi < own_end) hi = own_end;
         if (lo >= hi) continue;
 
-        float win[W > 1 ? W - 1 : 1][VEC], old[W > 1 ? W - 1 : 1][VEC];
+        float win[W > 1 ? W - 1 : 1][VEC];
+        int32_t from = -1;
         if (owner) {
-            const int32_t slot = a.state ? seq_slot(a.seq, a.seq.from, i) : -1;
+            from = a.state ? seq_slot(a.seq, a.seq.from, i) : -1;
 #pragma unroll
             for (int k = 0; k < W - 1; k++) {
 #pragma unroll
-                for (int j = 0; j < VEC; j++) old[k][j] = 0.0f;
-                if (slot >= 0) load_row<VEC>(state + slot * a.slot_stride + (int64_t)k * a.channels, nv, old[k]);
-#pragma unroll
-                for (int j = 0; j < VEC; j++) win[k][j] = old[k][j];
+                for (int j = 0; j < VEC; j++) win[k][j] = 0.0f;
+                if (from >= 0) load_row<VEC>(state + from * a.slot_stride + (int64_t)k * a.channels, nv, win[k]);
             }
         } else {
 #pragma unroll
             for (int k = 0; k < W - 1; k++) load_row<VEC>(in + (int64_t)(lo - (W - 1) + k) * a.in_stride, nv, win[k]);
         }
-        for (int32_t t = lo; t < hi; t++) {
-            float x[VEC], y[VEC];
-            load_row<VEC>(in + (int64_t)t * a.in_stride, nv, x);
+        // AHEAD rows on their way at once; past the end the last one again
+        for (int32_t t0 = lo; t0 < hi; t0 += AHEAD) {
+            Row q[AHEAD];
 #pragma unroll
-            for (int j = 0; j < VEC; j++) {
-                float s = bias[j];
+            for (int u = 0; u < AHEAD; u++) q[u].load(in + (int64_t)(t0 + u < hi ? t0 + u : hi - 1) * a.in_stride, nv);
 #pragma unroll
-                for (int k = 0; k < W - 1; k++) s = fmaf(w[k][j], win[k][j], s);
-                s = fmaf(w[W - 1][j], x[j], s);
-                y[j] = a.silu ? silu(s) : s;
-            }
-            store_row<VEC>(out + (int64_t)t * a.out_stride, nv, y);
-            if constexpr (W > 1) {
+            for (int u = 0; u < AHEAD; u++) {
+                if (t0 + u >= hi) break;
+                float x[VEC], y[VEC];
 #pragma unroll
-                for (int k = 0; k + 1 < W - 1; k++)
+                for (int j = 0; j < VEC; j++) x[j] = q[u].get(j);
 #pragma unroll
-                    for (int j = 0; j < VEC; j++) win[k][j] = win[k + 1][j];
+                for (int j = 0; j < VEC; j++) {
+                    float s = bias[j];
 #pragma unroll
-                for (int j = 0; j < VEC; j++) win[W - 2][j] = x[j];
+                    for (int k = 0; k < W - 1; k++) s = fmaf(w[k][j], win[k][j], s);
+                    y[j] = fmaf(w[W - 1][j], x[j], s);
+                }
+                if (a.silu)
+#pragma unroll
+                    for (int j = 0; j < VEC; j++) y[j] = silu(y[j]);
+                store_row<VEC>(out + (int64_t)(t0 + u) * a.out_stride, nv, y);
+                if constexpr (W > 1) {
+#pragma unroll
+                    for (int k = 0; k + 1 < W - 1; k++)
+#pragma unroll
+                        for (int j = 0; j < VEC; j++) win[k][j] = win[k + 1][j];
+#pragma unroll
+                    for (int j = 0; j < VEC; j++) win[W - 2][j] = x[j];
+                }
             }
         }
         const int32_t slot = owner && a.state ? seq_slot(a.seq, a.seq.to, i) : -1;
@@ -112,33 +139,35 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
             for (int k = 0; k < W - 1; k++) {
                 const int32_t at = e - b - (W - 1) + k;  // the sequence's row that becomes state row k; below 0 an old one
                 float v[VEC];
-                if (at >= 0) {
-                    load_row<VEC>(in + (int64_t)(b + at) * a.in_stride, nv, v);
-                } else {
 #pragma unroll
-                    for (int j = 0; j < VEC; j++) v[j] = 0.0f;
-#pragma unroll
-                    for (int q = 1; q < W - 1; q++)
-                        if (q == W - 1 + at)
-#pragma unroll
-                            for (int j = 0; j < VEC; j++) v[j] = old[q][j];
-                }
+                for (int j = 0; j < VEC; j++) v[j] = 0.0f;
+                // an old row moves down, and none is overwritten before it has
+                if (at >= 0) load_row<VEC>(in + (int64_t)(b + at) * a.in_stride, nv, v);
+                else if (from >= 0) load_row<VEC>(state + from * a.slot_stride + (int64_t)(W - 1 + at) * a.channels, nv, v);
                 store_row<VEC>(state + slot * a.slot_stride + (int64_t)k * a.channels, nv, v);
             }
         }
     }
 }
 
+// Rows per run: 32, and fewer until there are 2048 wavefronts (two for every SIMD): a run reads taps - 1 rows more
+// than it computes (12347 rows, 4096 channels: 50.4 us with 32, 52.5 with 16; 32 alone would leave 64 rows of 2048 channels to 16 wavefronts).
 template <typename T, int W>
 static int launch(ConvArgs a, hipStream_t s)
 {
-    constexpr int VEC = 16 / sizeof(T);
+    constexpr int VEC = 8 / sizeof(T);
     a.vecs = (a.channels + VEC - 1) / VEC;
-    a.run = a.seq.start || a.seq.each > 1 ? 16 : 1;
-    const int64_t threads = (int64_t)a.vecs * ((a.seq.tokens + a.run - 1) / a.run);
+    const bool single = !a.seq.start && a.seq.each == 1;
+    int64_t threads = 0;
+    for (a.run = single ? 1 : 32;; a.run /= 2) {
+        threads = (int64_t)a.vecs * (((int64_t)a.seq.tokens + a.run - 1) / a.run);
+        if (a.run <= 4 || threads >= 2048 * 64) break;
+    }
     const int64_t blocks = (threads + 255) / 256;
-    if (blocks > INT32_MAX) return ICV_ERR_INVALID_ARG;
-    k_causal_conv<T, W, VEC><<<(uint32_t)blocks, 256, 0, s>>>(a);
+    if (blocks > INT32_MAX - 8) return ICV_ERR_INVALID_ARG;
+    a.per_xcd = (int32_t)((blocks + 7) / 8);
+    if (single) k_causal_conv<T, W, VEC, 1><<<8 * a.per_xcd, 256, 0, s>>>(a);
+    else k_causal_conv<T, W, VEC, 4><<<8 * a.per_xcd, 256, 0, s>>>(a);
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;
 }

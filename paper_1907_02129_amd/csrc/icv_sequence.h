@@ -18,6 +18,7 @@ struct SeqArgs {
 inline int make_seq_args(const icv_sequences* s, int32_t slots, SeqArgs* a)
 {
     if (!s || s->count < 0 || s->tokens < 0) return ICV_ERR_INVALID_ARG;
+    if (s->tokens > INT32_MAX - 65536) return ICV_ERR_UNSUPPORTED;      // row numbers past a tile's end stay in 32 bits
     if (!s->start && s->count > 0 && s->tokens % s->count != 0) return ICV_ERR_INVALID_ARG;
     for (const int32_t* q : {s->start, s->length, s->from, s->to})
         if ((uintptr_t)q & 3u) return ICV_ERR_INVALID_ARG;
@@ -83,6 +84,29 @@ __device__ inline void store_row(T* p, int n, const float (&v)[N])
             if (j < n) p[j] = (T)v[j];
     }
 }
+
+// N neighbouring elements (16 bytes) on their way to registers, held as loaded: taken apart where they are loaded, they
+// would be waited for there.
+template <typename T, int N>
+struct RawRow {
+    uint32_t w[N * sizeof(T) / 4];
+    __device__ float get(int j) const
+    {
+        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[j]);
+        else return __builtin_bit_cast(float, j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    }
+    __device__ void load(const T* p, int n)
+    {
+        if (n >= N) {
+            __builtin_memcpy(w, p, sizeof(w));
+        } else {
+            T r[N];
+#pragma unroll
+            for (int j = 0; j < N; j++) r[j] = j < n ? p[j] : (T)0.0f;
+            __builtin_memcpy(w, r, sizeof(w));
+        }
+    }
+};
 
 // v / (1 + exp(-v)).  exp(-v) overflows to infinity below -88, which gives -0, the limit; the reciprocal is the
 // hardware's, within 1 ulp, next to an output rounding of at least that.

@@ -68,6 +68,7 @@ def test_sequences_that_make_no_sense_are_refused(lib, call):
         assert call(lib, s) == BAD
     for s in (seq(0, 8), seq(2, 0), seq(0, 0)):
         assert call(lib, s) == OK
+    assert call(lib, seq(1, 2 ** 31 - 1)) == UNSUPPORTED
     p = icv.make_causal_conv_params(16, 4)
     assert lib.icv_causal_conv1d(p, None, ADDRESS, ADDRESS, None, None, ADDRESS + 64, None) == BAD
 
