@@ -359,7 +359,8 @@ ICV_API int icv_selective_scan(const icv_scan_params* p, const icv_sequences* se
  *   infinite, infinite elements become NaN and the others zeros.
  * block_rows = 1 is for activations (a row's scales do not depend on the other rows), 128 for filters.
  *   input : [rows] rows of in_row_stride elements, only their element's alignment
- *   codes : [rows] rows of code_row_stride bytes, 16-byte aligned; all ceil(depth/128)*128 bytes of a row are written
+ *   codes : [rows] rows of code_row_stride bytes, 16-byte aligned, not over the input; all ceil(depth/128)*128 bytes of a
+ *           row are written
  *   scales: [ceil(depth/128)][ceil(rows/block_rows)] floats
  */
 typedef struct icv_quantize_params {
@@ -379,7 +380,7 @@ ICV_API int icv_quantize_fp8(const icv_quantize_params* p, const void* input, vo
  * bits below the largest of its 8 neighbours (about 1.5e-5 of the result).  rows = 0: nothing to do, ICV_OK.
  *   a, b  : 16-byte aligned; a_scales [ceil(depth/128)][rows], b_scales [ceil(depth/128)][ceil(cols/128)]
  *   bias  : cols floats or NULL
- *   out   : [rows] rows of out_row_stride elements: float (ICV_OUT_ACC) or bfloat16 (ICV_OUT_BF16)
+ *   out   : [rows] rows of out_row_stride elements, not over a or b: float (ICV_OUT_ACC) or bfloat16 (ICV_OUT_BF16)
  */
 typedef struct icv_matmul_params {
     int32_t rows, cols, depth;

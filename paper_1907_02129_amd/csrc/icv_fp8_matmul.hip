@@ -145,8 +145,9 @@ __device__ inline void copy4_global_to_lds(const void* sbase, uint32_t voff, uin
 // instruction's lanes read side by side lie in different banks; the permutation is made by the lanes' choice of
 // what to fetch.  A wavefront keeps its rows of a in registers for the stage and passes over its columns; a product is
 // scaled and added LAG instructions after its own, while those run.
-// A workgroup barrier that waits for nothing else: __syncthreads() also waits for every LDS read under way.
-__device__ inline void barrier() { asm volatile("s_barrier" : : : "memory"); }
+// A workgroup barrier behind this wavefront's LDS reads: what they read may be overwritten after it.  Copies to LDS that
+// are still on their way are not waited for.
+__device__ inline void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
 // Rows of a wavefront's MW x NW outputs that its part of LDS takes at a time.
 template <typename OUT>
@@ -468,6 +469,7 @@ extern "C" int icv_matmul_fp8(const icv_matmul_params* p, const void* a, const f
     const auto off = [](const void* q, uintptr_t bytes) { return ((uintptr_t)q & (bytes - 1)) != 0; };
     if (off(a, 16) || off(b, 16) || off(a_scales, 4) || off(b_scales, 4) || off(bias, 4) || off(out, p->out_type == ICV_OUT_ACC ? 4 : 2))
         return ICV_ERR_INVALID_ARG;
+    if (out == a || out == b) return ICV_ERR_INVALID_ARG;
     MatmulArgs g = {(const uint8_t*)a, (const uint8_t*)b, a_scales, b_scales, bias, out, p->rows, p->cols, blocks, (p->cols + 127) / 128,
                     p->a_row_stride ? p->a_row_stride : (int64_t)blocks * 128, p->b_row_stride ? p->b_row_stride : (int64_t)blocks * 128,
                     p->out_row_stride ? p->out_row_stride : p->cols};

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void k_quantize_blocks(QuantArgs a)
     __shared__ float part[4];
     const int tid = threadIdx.x;
     const int32_t block = (int32_t)(blockIdx.x % a.blocks), strip = (int32_t)(blockIdx.x / a.blocks);
-    const int32_t c = block * 128 + (tid & 15) * 8, row_blocks = (a.rows + 127) / 128;
+    const int32_t c = block * 128 + (tid & 15) * 8, row_blocks = (a.rows - 1) / 128 + 1;
     const int n = a.depth - c < 0 ? 0 : (a.depth - c < 8 ? a.depth - c : 8);
     float v[8][8], m = 0.0f;
 #pragma unroll
@@ -143,11 +143,11 @@ static int launch(const QuantArgs& a, int block_rows, hipStream_t s)
 {
     if (block_rows == 1) {
         constexpr int R = 2;       // 12288 x 4096 bfloat16: 32.3 us, 35.6 with four rows, 44.7 with eight
-        const int64_t waves = (int64_t)((a.blocks + 3) / 4) * ((a.rows + R - 1) / R), n = (waves + 3) / 4;
+        const int64_t waves = (int64_t)((a.blocks + 3) / 4) * ((a.rows - 1) / R + 1), n = (waves + 3) / 4;
         if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
         k_quantize_rows<T, R><<<(uint32_t)n, 256, 0, s>>>(a);
     } else {
-        const int64_t n = (int64_t)a.blocks * ((a.rows + 127) / 128);
+        const int64_t n = (int64_t)a.blocks * ((a.rows - 1) / 128 + 1);
         if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
         k_quantize_blocks<T><<<(uint32_t)n, 256, 0, s>>>(a);
     }
@@ -168,7 +168,8 @@ extern "C" int icv_quantize_fp8(const icv_quantize_params* p, const void* input,
     if (p->in_row_stride && p->in_row_stride < p->depth) return ICV_ERR_INVALID_ARG;
     if (p->code_row_stride && (p->code_row_stride % 16 != 0 || p->code_row_stride < (int64_t)blocks * 128)) return ICV_ERR_INVALID_ARG;
     if (p->rows == 0) return ICV_OK;
-    if (!input || !codes || !scales || misaligned(input, p->dtype == ICV_F32 ? 4 : 2) || misaligned(codes, 16) || misaligned(scales, 4))
+    if (!input || !codes || !scales || misaligned(input, p->dtype == ICV_F32 ? 4 : 2) || misaligned(codes, 16) || misaligned(scales, 4) ||
+        input == codes)
         return ICV_ERR_INVALID_ARG;
     QuantArgs a = {input, (uint8_t*)codes, scales, p->rows, p->depth, blocks,
                    p->in_row_stride ? p->in_row_stride : p->depth, p->code_row_stride ? p->code_row_stride : (int64_t)blocks * 128};

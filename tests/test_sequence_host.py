@@ -169,6 +169,8 @@ def test_pointers_of_the_8_bit_operators_are_checked(lib):
     assert quantize(lib, dtype=icv.ICV_U8I8) == UNSUPPORTED and quantize(lib, rows=0) == OK
     for name, odd in (("a", 8), ("a_scales", 2), ("b", 4), ("b_scales", 1), ("out", 1)):
         assert matmul(lib, {name: None}) == BAD and matmul(lib, {name: ADDRESS + odd}) == BAD
+    assert quantize(lib, {"codes": ADDRESS}) == BAD                                     # over their inputs
+    assert matmul(lib, {"out": ADDRESS}) == BAD and matmul(lib, {"out": ADDRESS + 8192}) == BAD
     assert matmul(lib, {"bias": ADDRESS + 1}) == BAD and matmul(lib, rows=0) == OK
     assert matmul(lib, {"out": ADDRESS + 2}, out_type=icv.ICV_OUT_ACC) == BAD
     assert lib.icv_quantize_fp8(None, ADDRESS, ADDRESS, ADDRESS, None) == BAD
