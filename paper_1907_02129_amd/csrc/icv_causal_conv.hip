@@ -28,10 +28,11 @@ struct ConvArgs {
     SeqArgs seq;
 };
 
-template <typename T, int W, int VEC, int AHEAD>
+template <typename T, int W, int VEC, int AHEAD, bool ODD>
 __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
 {
-    using Row = RawRow<T, VEC>;
+    using Row = Raw<T, VEC, ODD>;
+    const auto take = [](Row& q, const T* p, int n) { q.load((const uint8_t*)p, 0, n); };
     // workgroups go to the 8 XCDs in turn: each gets neighbouring runs, so that the rows in front of a run are in its L2
     const int64_t id = ((int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3)) * 256 + threadIdx.x;
     const int32_t runs = (a.seq.tokens - 1) / a.run + 1;
@@ -49,15 +50,15 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
         // the filter's rows of these channels lie side by side
         const T* f = (const T*)a.filt + (int64_t)c0 * W;
         T q[VEC * W];
-        if (nv == VEC) {
+        if (!ODD) {
             __builtin_memcpy(q, f, sizeof(q));
         } else {
 #pragma unroll
-            for (int j = 0; j < VEC * W; j++) q[j] = j < nv * W ? f[j] : (T)0.0f;
+            for (int j = 0; j < VEC * W; j++) q[j] = f[j < nv * W ? j : 0];
         }
 #pragma unroll
         for (int j = 0; j < VEC; j++) {
-            bias[j] = a.bias && j < nv ? a.bias[c0 + j] : 0.0f;
+            bias[j] = a.bias ? a.bias[c0 + (!ODD || j < nv ? j : 0)] : 0.0f;
 #pragma unroll
             for (int k = 0; k < W; k++) w[k][j] = (float)q[j * W + k];
         }
@@ -89,23 +90,24 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
 
         float win[W > 1 ? W - 1 : 1][VEC];
         int32_t from = -1;
+        Row q[AHEAD > W - 1 ? AHEAD : W - 1];
         if (owner) {
             from = a.state ? seq_slot(a.seq, a.seq.from, i) : -1;
+            if (from >= 0)
 #pragma unroll
-            for (int k = 0; k < W - 1; k++) {
-#pragma unroll
-                for (int j = 0; j < VEC; j++) win[k][j] = 0.0f;
-                if (from >= 0) load_row<VEC>(state + from * a.slot_stride + (int64_t)k * a.channels, nv, win[k]);
-            }
+                for (int k = 0; k < W - 1; k++) take(q[k], state + from * a.slot_stride + (int64_t)k * a.channels, nv);
         } else {
 #pragma unroll
-            for (int k = 0; k < W - 1; k++) load_row<VEC>(in + (int64_t)(lo - (W - 1) + k) * a.in_stride, nv, win[k]);
+            for (int k = 0; k < W - 1; k++) take(q[k], in + (int64_t)(lo - (W - 1) + k) * a.in_stride, nv);
         }
+#pragma unroll
+        for (int k = 0; k < W - 1; k++)
+#pragma unroll
+            for (int j = 0; j < VEC; j++) win[k][j] = owner && from < 0 ? 0.0f : q[k].get(j);
         // AHEAD rows on their way at once; past the end the last one again
         for (int32_t t0 = lo; t0 < hi; t0 += AHEAD) {
-            Row q[AHEAD];
 #pragma unroll
-            for (int u = 0; u < AHEAD; u++) q[u].load(in + (int64_t)(t0 + u < hi ? t0 + u : hi - 1) * a.in_stride, nv);
+            for (int u = 0; u < AHEAD; u++) take(q[u], in + (int64_t)(t0 + u < hi ? t0 + u : hi - 1) * a.in_stride, nv);
 #pragma unroll
             for (int u = 0; u < AHEAD; u++) {
                 if (t0 + u >= hi) break;
@@ -122,7 +124,7 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
                 if (a.silu)
 #pragma unroll
                     for (int j = 0; j < VEC; j++) y[j] = silu(y[j]);
-                store_row<VEC>(out + (int64_t)(t0 + u) * a.out_stride, nv, y);
+                store_row<VEC>(out + (int64_t)(t0 + u) * a.out_stride, ODD ? nv : VEC, y);
                 if constexpr (W > 1) {
 #pragma unroll
                     for (int k = 0; k + 1 < W - 1; k++)
@@ -142,9 +144,14 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
 #pragma unroll
                 for (int j = 0; j < VEC; j++) v[j] = 0.0f;
                 // an old row moves down, and none is overwritten before it has
-                if (at >= 0) load_row<VEC>(in + (int64_t)(b + at) * a.in_stride, nv, v);
-                else if (from >= 0) load_row<VEC>(state + from * a.slot_stride + (int64_t)(W - 1 + at) * a.channels, nv, v);
-                store_row<VEC>(state + slot * a.slot_stride + (int64_t)k * a.channels, nv, v);
+                const T* p = at >= 0 ? in + (int64_t)(b + at) * a.in_stride
+                                     : (from >= 0 ? state + from * a.slot_stride + (int64_t)(W - 1 + at) * a.channels : nullptr);
+                if (p) {
+                    take(q[0], p, nv);
+#pragma unroll
+                    for (int j = 0; j < VEC; j++) v[j] = q[0].get(j);
+                }
+                store_row<VEC>(state + slot * a.slot_stride + (int64_t)k * a.channels, ODD ? nv : VEC, v);
             }
         }
     }
@@ -166,8 +173,11 @@ static int launch(ConvArgs a, hipStream_t s)
     const int64_t blocks = (threads + 255) / 256;
     if (blocks > INT32_MAX - 8) return ICV_ERR_INVALID_ARG;
     a.per_xcd = (int32_t)((blocks + 7) / 8);
-    if (single) k_causal_conv<T, W, VEC, 1><<<8 * a.per_xcd, 256, 0, s>>>(a);
-    else k_causal_conv<T, W, VEC, 4><<<8 * a.per_xcd, 256, 0, s>>>(a);
+    const bool odd = a.channels % VEC != 0;
+    if (single && odd) k_causal_conv<T, W, VEC, 1, true><<<8 * a.per_xcd, 256, 0, s>>>(a);
+    else if (single) k_causal_conv<T, W, VEC, 1, false><<<8 * a.per_xcd, 256, 0, s>>>(a);
+    else if (odd) k_causal_conv<T, W, VEC, 4, true><<<8 * a.per_xcd, 256, 0, s>>>(a);
+    else k_causal_conv<T, W, VEC, 4, false><<<8 * a.per_xcd, 256, 0, s>>>(a);
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;
 }

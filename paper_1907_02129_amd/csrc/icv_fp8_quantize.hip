@@ -2,7 +2,7 @@
 //
 // Memory bound: every element is read once and leaves as one byte.  Sixteen lanes take a row's block of 128, 8 elements
 // each, so the maximum of a row's block is four exchanges within a row of 16 lanes, and a wavefront covers four
-// neighbouring blocks of a row.  12288 x 4096 from bfloat16: 32.3 us, 4.7 TB/s (a copy: 5.2).
+// neighbouring blocks of a row.  12288 x 4096 from bfloat16: 31.7 us, 4.8 TB/s (a copy: 5.2).
 #include "icv_sequence.h"
 
 namespace icv {
@@ -73,7 +73,7 @@ __device__ inline uint2 encode8(const float (&v)[8], const Divider& by)
 }
 
 // A wavefront takes R rows of four neighbouring blocks of columns.
-template <typename T, int R>
+template <typename T, int R, bool ODD>
 __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -85,15 +85,16 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a)
     const int32_t r0 = (int32_t)(strip * R), c = block * 128 + (lane & 15) * 8;
     const int n = a.depth - c < 0 ? 0 : (a.depth - c < 8 ? a.depth - c : 8);
     float scale[R];
-    RawRow<T, 8> raw[R];
+    Raw<T, 8, ODD> raw[R];
 #pragma unroll
-    for (int r = 0; r < R; r++) raw[r].load((const T*)a.in + (int64_t)(r0 + r < a.rows ? r0 + r : r0) * a.in_stride + (n ? c : 0), n);
+    for (int r = 0; r < R; r++)
+        raw[r].load((const uint8_t*)((const T*)a.in + (int64_t)(r0 + r < a.rows ? r0 + r : r0) * a.in_stride + (n ? c : 0)), 0, n);
 #pragma unroll
     for (int r = 0; r < R; r++) {
         float v[8], m = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            v[j] = raw[r].get(j);
+            v[j] = (ODD ? j < n : n > 0) ? raw[r].get(j) : 0.0f;
             m = fmaxf(m, fabsf(v[j]));
         }
         scale[r] = scale_of(row16_max(m));
@@ -106,7 +107,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a)
 }
 
 // A workgroup takes a block of 128 x 128: 16 rows at a time, 8 elements a lane, all held until the maximum is known.
-template <typename T>
+template <typename T, bool ODD>
 __global__ __launch_bounds__(256) void k_quantize_blocks(QuantArgs a)
 {
     __shared__ float part[4];
@@ -114,15 +115,18 @@ __global__ __launch_bounds__(256) void k_quantize_blocks(QuantArgs a)
     const int32_t block = (int32_t)(blockIdx.x % a.blocks), strip = (int32_t)(blockIdx.x / a.blocks);
     const int32_t c = block * 128 + (tid & 15) * 8, row_blocks = (a.rows - 1) / 128 + 1;
     const int n = a.depth - c < 0 ? 0 : (a.depth - c < 8 ? a.depth - c : 8);
-    float v[8][8], m = 0.0f;
+    Raw<T, 8, ODD> raw[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const int64_t r = (int64_t)strip * 128 + i * 16 + (tid >> 4);
-        const bool in = r < a.rows && n > 0;
-        load_row<8>((const T*)a.in + (in ? r * a.in_stride + c : 0), in ? n : 0, v[i]);
-#pragma unroll
-        for (int j = 0; j < 8; j++) m = fmaxf(m, fabsf(v[i][j]));
+        raw[i].load((const uint8_t*)((const T*)a.in + (r < a.rows ? r : a.rows - 1) * a.in_stride + (n ? c : 0)), 0, n);
     }
+    float m = 0.0f;
+    const auto value = [&](int i, int j) { return (ODD ? j < n : n > 0) ? raw[i].get(j) : 0.0f; };      // rows past the end: the last again
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int j = 0; j < 8; j++) m = fmaxf(m, fabsf(value(i, j)));
     m = row16_max(m);
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
@@ -133,7 +137,10 @@ __global__ __launch_bounds__(256) void k_quantize_blocks(QuantArgs a)
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const int64_t r = (int64_t)strip * 128 + i * 16 + (tid >> 4);
-        if (r < a.rows) *(uint2*)(a.codes + r * a.code_stride + c) = encode8(v[i], by);
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) v[j] = value(i, j);
+        if (r < a.rows) *(uint2*)(a.codes + r * a.code_stride + c) = encode8(v, by);
     }
     if (tid == 0) a.scales[(int64_t)block * row_blocks + strip] = scale;
 }
@@ -142,14 +149,16 @@ template <typename T>
 static int launch(const QuantArgs& a, int block_rows, hipStream_t s)
 {
     if (block_rows == 1) {
-        constexpr int R = 2;       // 12288 x 4096 bfloat16: 32.3 us, 35.6 with four rows, 44.7 with eight
+        constexpr int R = 2;       // 12288 x 4096 bfloat16: 31.7 us; 33.6 with one row, 31.4 with four, which leaves short batches fewer wavefronts
         const int64_t waves = (int64_t)((a.blocks + 3) / 4) * ((a.rows - 1) / R + 1), n = (waves + 3) / 4;
         if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-        k_quantize_rows<T, R><<<(uint32_t)n, 256, 0, s>>>(a);
+        if (a.depth % 8) k_quantize_rows<T, R, true><<<(uint32_t)n, 256, 0, s>>>(a);
+        else k_quantize_rows<T, R, false><<<(uint32_t)n, 256, 0, s>>>(a);
     } else {
         const int64_t n = (int64_t)a.blocks * ((a.rows - 1) / 128 + 1);
         if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-        k_quantize_blocks<T><<<(uint32_t)n, 256, 0, s>>>(a);
+        if (a.depth % 8) k_quantize_blocks<T, true><<<(uint32_t)n, 256, 0, s>>>(a);
+        else k_quantize_blocks<T, false><<<(uint32_t)n, 256, 0, s>>>(a);
     }
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;

@@ -43,33 +43,6 @@ __device__ inline float softplus(float v)
     return fmaxf(v, 0.0f) + fmaf(__builtin_amdgcn_logf(u), kLn2, e - (u - 1.0f));
 }
 
-// N neighbouring elements on their way to registers, held as loaded: taken apart where they are loaded, they would be waited
-// for there.  ODD: some may not be there (an odd group of channels, a number of states that is no multiple of 4), so each
-// is loaded by itself, from the last one that is there if need be.
-template <typename T, int N, bool ODD>
-struct Raw {
-    uint32_t w[ODD ? N : N * sizeof(T) / 4];
-    __device__ float get(int j) const
-    {
-        if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[j]);
-        else if constexpr (ODD) return __builtin_bit_cast(float, w[j] << 16);
-        else return __builtin_bit_cast(float, j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
-    }
-    __device__ void load(const uint8_t* base, uint32_t at, int n)       // n of them are there, or none
-    {
-        if constexpr (!ODD) {
-            __builtin_memcpy(w, base + at, sizeof(w));
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; j++) {
-                const uint8_t* p = base + at + (j < n ? j : 0) * sizeof(T);
-                if constexpr (sizeof(T) == 4) w[j] = *(const uint32_t*)p;
-                else w[j] = *(const uint16_t*)p;
-            }
-        }
-    }
-};
-
 // lane -> its place among the S lanes of a channel, and the channel among the wavefront's.  The four lowest states of a
 // channel sit in one quad; with 8 lanes the second quad is 8 lanes away, with 16 all of a row of 16 is one channel's,
 // so that the sums over quads are rotations within a row.
@@ -398,47 +371,70 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
     }
 }
 
-// One row per sequence: the state is read and written once, which is what bounds it (128 sequences, 4096 channels, 16 states, bfloat16:
-// 18.5 us, 3.8 TB/s; two or four sequences per workgroup, their states on their way together, 19.8 and 21.1).
-template <typename T, int S>
+// One row per sequence: the state is read and written once, which is what bounds it.  A workgroup takes its channels of Q
+// sequences: a wavefront alone waits for the slot number, then for the state, then ends; with Q states on their way together
+// the compute units' wavefronts cover that: 128 sequences, 4096 channels, 16 states, bfloat16 15.8 us, 4.5 TB/s, with two; 16.8 with
+// one, 16.1 with four.  Loads have no branches around them (a sequence that continues no slot reads slot 0 and
+// drops it; 18.5 us with branches).
+template <typename T, int S, bool ODD, int Q>
 __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
 {
     constexpr int CW = 256 / S;
     const int tid = threadIdx.x, lane = tid & 63;
     const int32_t tiles = (a.channels + CW - 1) / CW;
-    const int32_t tile = (int32_t)(blockIdx.x % tiles), i = (int32_t)(blockIdx.x / tiles);
-    if (seq_end(a.seq, i, i) == i) return;
+    const int32_t tile = (int32_t)(blockIdx.x % tiles), i0 = (int32_t)(blockIdx.x / tiles) * Q;
     int s, wch;
     lane_place<S>(lane, &s, &wch);
     const int32_t d = tile * CW + (tid >> 6) * (64 / S) + wch;
     if (d >= a.channels) return;                      // whole channels, so whole exchange partners
     const int nv = a.states - 4 * s < 0 ? 0 : (a.states - 4 * s < 4 ? a.states - 4 * s : 4);
-    const int64_t state_at = (int64_t)d * a.states + 4 * s, bc = (int64_t)(d / a.per_group) * a.states + 4 * s;
-    const int32_t src = a.state ? seq_slot(a.seq, a.seq.from, i) : -1, dst = a.state ? seq_slot(a.seq, a.seq.to, i) : -1;
+    const uint32_t n4 = nv ? 4 * s : 0;
+    const int64_t state_at = (int64_t)d * a.states + n4, bc = (int64_t)(d / a.per_group) * a.states + n4;
+    const bool slots = a.state && a.seq.slots > 0;
 
-    float A[4], h[4] = {0.0f, 0.0f, 0.0f, 0.0f}, b[4], c[4];
-    if (src >= 0) load_states(a.state + src * a.slot_stride + state_at, nv, h);
-    load_states(a.A + state_at, nv, A);
-    load_row<4>((const T*)a.B + i * a.bs + bc, nv, b);
-    load_row<4>((const T*)a.C + i * a.cs + bc, nv, c);
-    const float x = (float)((const T*)a.x)[i * a.xs + d];
-    float dt = (float)((const T*)a.dt)[i * a.dts + d] + (a.dtb ? a.dtb[d] : 0.0f);
-    if (a.softplus) dt = softplus(dt);
-    float y = 0.0f;
+    int32_t seq[Q], src[Q], dst[Q];
+    bool on[Q];
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-        h[j] = fmaf(__builtin_amdgcn_exp2f(dt * A[j] * kLog2e), h[j], dt * x * b[j]);
-        if (j < nv) y = fmaf(c[j], h[j], y);
+    for (int q = 0; q < Q; q++) {
+        seq[q] = i0 + q < a.seq.count ? i0 + q : i0;
+        on[q] = i0 + q < a.seq.count && seq_end(a.seq, seq[q], seq[q]) != seq[q];
+        src[q] = slots ? seq_slot(a.seq, a.seq.from, seq[q]) : -1;
+        dst[q] = slots && on[q] ? seq_slot(a.seq, a.seq.to, seq[q]) : -1;
     }
-    if (dst >= 0) store_row<4>(a.state + dst * a.slot_stride + state_at, nv, h);
-    if (S >= 2) y += dpp<kXor1>(y);
-    if (S >= 4) y += dpp<kXor2>(y);
-    if (S == 16) y += dpp<kRotate4>(y);
-    if (S >= 8) y += dpp<kRotate8>(y);
-    if (s == 0) {
-        if (a.D) y = fmaf(a.D[d], x, y);
-        if (a.z) y *= silu((float)((const T*)a.z)[i * a.zs + d]);
-        ((T*)a.out)[i * a.os + d] = (T)y;
+    Raw<float, 4, ODD> hr[Q], Ar;
+    Raw<T, 4, ODD> br[Q], cr[Q];
+    Raw<T, 1, false> xr[Q], dr[Q], zr[Q];
+    const auto at = [](const void* p, int64_t element, size_t size) { return (const uint8_t*)p + element * (int64_t)size; };
+    Ar.load(at(a.A, state_at, 4), 0, nv);
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        if (slots) hr[q].load(at(a.state, (src[q] >= 0 ? src[q] : 0) * a.slot_stride + state_at, 4), 0, nv);
+        br[q].load(at(a.B, seq[q] * a.bs + bc, sizeof(T)), 0, nv);
+        cr[q].load(at(a.C, seq[q] * a.cs + bc, sizeof(T)), 0, nv);
+        xr[q].load(at(a.x, seq[q] * a.xs + d, sizeof(T)), 0, 1);
+        dr[q].load(at(a.dt, seq[q] * a.dts + d, sizeof(T)), 0, 1);
+        if (a.z) zr[q].load(at(a.z, seq[q] * a.zs + d, sizeof(T)), 0, 1);
+    }
+    const float dtb = a.dtb ? a.dtb[d] : 0.0f, D = a.D ? a.D[d] : 0.0f;
+#pragma unroll
+    for (int q = 0; q < Q; q++) {
+        float dt = dr[q].get(0) + dtb, y = 0.0f, h[4];
+        const float x = xr[q].get(0);
+        if (a.softplus) dt = softplus(dt);
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const float old = src[q] >= 0 ? hr[q].get(j) : 0.0f;
+            h[j] = fmaf(__builtin_amdgcn_exp2f(dt * Ar.get(j) * kLog2e), old, dt * x * br[q].get(j));
+            if (!ODD || j < nv) y = fmaf(cr[q].get(j), h[j], y);
+        }
+        if (dst[q] >= 0) store_row<4>(a.state + dst[q] * a.slot_stride + state_at, nv, h);
+        if (S >= 2) y += dpp<kXor1>(y);
+        if (S >= 4) y += dpp<kXor2>(y);
+        if (S == 16) y += dpp<kRotate4>(y);
+        if (S >= 8) y += dpp<kRotate8>(y);
+        if (a.D) y = fmaf(D, x, y);
+        if (a.z) y *= silu(zr[q].get(0));
+        if (s == 0 && on[q]) ((T*)a.out)[seq[q] * a.os + d] = (T)y;
     }
 }
 
@@ -480,9 +476,14 @@ static int launch(const ScanArgs& a, bool step, int64_t pieces, hipStream_t s)
     constexpr int CW = 256 / S;
     const bool odd = a.states != 4 * S || a.per_group % 2 != 0;
     if (step) {
-        const int64_t n = (int64_t)((a.channels + CW - 1) / CW) * a.seq.count;
+        const int64_t tiles = (a.channels + CW - 1) / CW;
+        const int64_t wgs = tiles * a.seq.count;
+        const bool two = wgs >= 2048 && a.states == 4 * S;      // more than the chip holds at once
+        const int64_t n = two ? tiles * (((int64_t)a.seq.count + 1) / 2) : wgs;
         if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-        k_scan_step<T, S><<<(uint32_t)n, 256, 0, s>>>(a);
+        if (a.states != 4 * S) k_scan_step<T, S, true, 1><<<(uint32_t)n, 256, 0, s>>>(a);
+        else if (two) k_scan_step<T, S, false, 2><<<(uint32_t)n, 256, 0, s>>>(a);
+        else k_scan_step<T, S, false, 1><<<(uint32_t)n, 256, 0, s>>>(a);
         ICV_HIP_CHECK(hipGetLastError());
         return ICV_OK;
     }

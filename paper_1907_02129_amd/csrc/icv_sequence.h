@@ -85,25 +85,30 @@ __device__ inline void store_row(T* p, int n, const float (&v)[N])
     }
 }
 
-// N neighbouring elements (16 bytes) on their way to registers, held as loaded: taken apart where they are loaded, they
-// would be waited for there.
-template <typename T, int N>
-struct RawRow {
-    uint32_t w[N * sizeof(T) / 4];
+// N neighbouring elements on their way to registers, held as loaded: taken apart where they are loaded, they would be waited
+// for there, and a branch around a load makes them wait behind it.  ODD: some may not be there (an odd width), so each is loaded by itself,
+// one that is not from the first one's place, which must be there.
+template <typename T, int N, bool ODD>
+struct Raw {
+    static constexpr bool WORDS = !ODD && N * sizeof(T) >= 4;
+    uint32_t w[WORDS ? N * sizeof(T) / 4 : N];
     __device__ float get(int j) const
     {
         if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[j]);
+        else if constexpr (!WORDS) return __builtin_bit_cast(float, w[j] << 16);
         else return __builtin_bit_cast(float, j & 1 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
     }
-    __device__ void load(const T* p, int n)
+    __device__ void load(const uint8_t* base, uint32_t at, int n)       // n of them are there, or none
     {
-        if (n >= N) {
-            __builtin_memcpy(w, p, sizeof(w));
+        if constexpr (WORDS) {
+            __builtin_memcpy(w, base + at, sizeof(w));
         } else {
-            T r[N];
 #pragma unroll
-            for (int j = 0; j < N; j++) r[j] = j < n ? p[j] : (T)0.0f;
-            __builtin_memcpy(w, r, sizeof(w));
+            for (int j = 0; j < N; j++) {
+                const uint8_t* p = base + at + (j < n ? j : 0) * sizeof(T);
+                if constexpr (sizeof(T) == 4) w[j] = *(const uint32_t*)p;
+                else w[j] = *(const uint16_t*)p;
+            }
         }
     }
 };
