@@ -6,14 +6,15 @@
 // channels, 16 states, bfloat16 with gate: 290 us, of which the instructions alone take 250 (525 us at first: what was in the way
 // were waits for the next tile's loads inside conversions and branches, 64-bit address products, and bank conflicts).
 //
-// A lane keeps 4 states of a channel in registers, S lanes (1..16) a channel: the rows' delta and delta * x are then read
-// from LDS once for 4 states, and a channel's states take few enough registers for several workgroups on a compute
+// A lane keeps NS (4, 2 or 1) states of a channel in registers, S lanes (1..16) a channel: the rows' delta and delta * x are then
+// read from LDS once for NS states, and a channel's states take few enough registers for several workgroups on a compute
 // unit, whose wavefronts hide each other's latencies.  A workgroup of 256 lanes owns 256 / S channels of one group
 // (they share B and C) and walks a sequence in tiles of TT rows: the next tile's inputs are on their way from memory
 // while this one's rows are stepped through from LDS; softplus and the products with x are computed once per row and
 // channel when a tile is staged, and D * x and the gate once when it is stored.  The sums over a channel's lanes are
 // taken for four rows at a time, by exchanges inside quads that leave each lane with one row's sum.
 #include "icv_sequence.h"
+#include <cmath>
 
 namespace icv {
 
@@ -82,12 +83,6 @@ __device__ inline void reduce_rows(const float (&p)[4], int s, float (&y)[4])
     }
 }
 
-// The states a lane holds: n..n+3 of channel d, `nv` of them real.
-__device__ inline void load_states(const float* p, int nv, float (&h)[4])
-{
-    load_row<4>(p, nv, h);
-}
-
 // The n-th of at most 64 sequences by length, longest first; the same for all lanes.  Workgroups start in the order of their
 // numbers, and a long sequence that starts last keeps a few compute units busy alone: 24 sequences of 12347 rows and 4096 channels
 // took 412 us as they came, 376 by length.
@@ -106,19 +101,21 @@ __device__ inline int32_t nth_longest(const SeqArgs& q, int32_t n, int lane)
     return __builtin_ctzll(__ballot(lane < q.count && rank == n));
 }
 
-// Two rows' values of a lane's channel and states.
+// Two rows' values of a lane's channel and NS states.
+template <int NS>
 struct Rows2 {
     float2 v[2];
-    float4 b[2], c[2];
+    float b[2][NS], c[2][NS];
 };
 
-template <typename T, int S, bool ODD, int MODE>
+template <typename T, int S, int NS, bool ODD, int MODE>
 __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
 {
     constexpr int CW = 256 / S, TT = 8 * S < 64 ? 8 * S : 64, PAIRS = CW / 2, RPT = TT * PAIRS / 256, ROWS = TT / RPT;
-    constexpr int BCV = (TT * S + 255) / 256;      // vectors of 4 states of B (and C) a thread stages
+    constexpr int NP = S * NS, VS = NP / 4;        // states with those that are not there, in vectors of 4
+    constexpr int BCV = (TT * VS + 255) / 256;     // vectors of B (and C) a thread stages
     __shared__ __align__(16) float2 dtx[TT][CW];    // delta and delta * x; the row's output takes delta's place
-    __shared__ float4 sB[TT][S], sC[MODE == SCAN_PIECE_STATE ? 1 : TT][S];
+    __shared__ __align__(16) float sB[TT][NP], sC[MODE == SCAN_PIECE_STATE ? 1 : TT][NP];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int32_t tiles = a.group_tiles * (a.channels / a.per_group);
@@ -131,17 +128,33 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
         end = seq_end(a.seq, i, begin);
         if (begin == end) return;
     } else {
-        // the sequence that piece `unit` belongs to, counting every sequence's pieces
-        int32_t left = unit;
-        for (i = 0;; i++) {
-            if (i == a.seq.count) return;
-            begin = seq_begin(a.seq, i);
-            end = seq_end(a.seq, i, begin);
-            pieces = (end - begin + a.chunk - 1) / a.chunk;
-            if (left < pieces) break;
-            left -= pieces;
+        // the sequence that piece `unit` belongs to, counting every sequence's pieces: 64 sequences at a time, one to a lane
+        int32_t left = unit, i0 = 0;
+        for (;; i0 += 64) {
+            if (i0 >= a.seq.count) return;
+            int32_t mine = 0;
+            if (i0 + lane < a.seq.count) {
+                const int32_t b = seq_begin(a.seq, i0 + lane);
+                mine = (seq_end(a.seq, i0 + lane, b) - b + a.chunk - 1) / a.chunk;
+            }
+            int32_t upto = mine;                      // pieces of the lanes up to this one
+#pragma unroll
+            for (int step = 1; step < 64; step *= 2) {
+                const int32_t before = __shfl_up(upto, step);
+                if (lane >= step) upto += before;
+            }
+            const int32_t all = __builtin_amdgcn_readlane(upto, 63);
+            if (left < all) {
+                const int at = __builtin_ctzll(__ballot(upto > left));
+                i = i0 + at;
+                pieces = __builtin_amdgcn_readlane(mine, at);
+                piece = left - (__builtin_amdgcn_readlane(upto, at) - pieces);
+                break;
+            }
+            left -= all;
         }
-        piece = left;
+        begin = seq_begin(a.seq, i);
+        end = seq_end(a.seq, i, begin);
         if (MODE == SCAN_PIECE_STATE && piece == pieces - 1) return;
     }
     const int32_t first_unit = unit - piece;
@@ -157,40 +170,40 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
     lane_place<S>(lane, &s, &wch);
     const int ch = (tid >> 6) * (64 / S) + wch;
     const int32_t d = c0 + (ch < cn ? ch : 0);
-    const int nv = a.states - 4 * s < 0 ? 0 : (a.states - 4 * s < 4 ? a.states - 4 * s : 4);
+    const int nv = a.states - NS * s < 0 ? 0 : (a.states - NS * s < NS ? a.states - NS * s : NS);
 
-    float A[4], h[4];
-    load_states(a.A + (int64_t)d * a.states + 4 * s, nv, A);
+    float A[NS], h[NS];
+    load_row<NS>(a.A + (int64_t)d * a.states + NS * s, nv, A);
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
+    for (int j = 0; j < NS; j++) {
         A[j] *= kLog2e;
         A[j] = A[j] < -3.0e38f ? -3.0e38f : A[j];     // rows past the end step by 0 * A, which has to be 0
     }
 
-    const int64_t state_at = (int64_t)d * a.states + 4 * s;
+    const int64_t state_at = (int64_t)d * a.states + NS * s;
     const int64_t plane = (int64_t)a.channels * a.states;
 #pragma unroll
-    for (int j = 0; j < 4; j++) h[j] = 0.0f;
+    for (int j = 0; j < NS; j++) h[j] = 0.0f;
     if (piece == 0 && !(MODE == SCAN_PIECE_OUT && pieces > 1)) {
         const int32_t slot = a.state ? seq_slot(a.seq, a.seq.from, i) : -1;
-        if (slot >= 0) load_states(a.state + slot * a.slot_stride + state_at, nv, h);
+        if (slot >= 0) load_row<NS>(a.state + slot * a.slot_stride + state_at, nv, h);
         // the slot may be written while the pieces' outputs are computed: those read the copy in the last piece's place
-        if (MODE == SCAN_PIECE_STATE && ch < cn) store_row<4>(a.ws_state + (first_unit + pieces - 1) * plane + state_at, nv, h);
+        if (MODE == SCAN_PIECE_STATE && ch < cn) store_row<NS>(a.ws_state + (first_unit + pieces - 1) * plane + state_at, nv, h);
     } else if (MODE == SCAN_PIECE_OUT) {
-        load_states(a.ws_state + (piece == 0 ? first_unit + pieces - 1 : first_unit) * plane + state_at, nv, h);
+        load_row<NS>(a.ws_state + (piece == 0 ? first_unit + pieces - 1 : first_unit) * plane + state_at, nv, h);
         for (int32_t q0 = 1; q0 < piece; q0 += 8) {
-            float sum[8], w[8][4];
+            float sum[8], w[8][NS];
 #pragma unroll
             for (int u = 0; u < 8; u++) {              // past the last: the first again, not used
                 const int32_t q = first_unit + (q0 + u < piece ? q0 + u : q0);
                 sum[u] = a.ws_sum[(int64_t)q * a.channels + d];
-                load_states(a.ws_state + q * plane + state_at, nv, w[u]);
+                load_row<NS>(a.ws_state + q * plane + state_at, nv, w[u]);
             }
 #pragma unroll
             for (int u = 0; u < 8; u++)
                 if (q0 + u < piece)
 #pragma unroll
-                    for (int j = 0; j < 4; j++) h[j] = fmaf(__builtin_amdgcn_exp2f(sum[u] * A[j]), h[j], w[u][j]);
+                    for (int j = 0; j < NS; j++) h[j] = fmaf(__builtin_amdgcn_exp2f(sum[u] * A[j]), h[j], w[u][j]);
         }
     }
 
@@ -212,8 +225,8 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
                    oo = vrow * (uint32_t)a.os + vc;
     const auto row_of = [](const void* p, int64_t row, int64_t stride) { return (const uint8_t*)p + row * stride * SZ; };      // scalar
     // Rows past the end repeat the last one (and are made to change nothing when they are staged): loads without branches
-    constexpr int BCT = TT * S < 256 ? TT * S : 256;               // threads with B and C of their own; the others repeat them
-    const int bct = tid % BCT, n4 = 4 * (bct % S), bcrow = bct / S;
+    constexpr int BCT = TT * VS < 256 ? TT * VS : 256;              // threads with B and C of their own; the others repeat them
+    const int bct = tid % BCT, n4 = 4 * (bct % VS), bcrow = bct / VS;
     const int bcn = a.states - n4 < 0 ? 0 : (a.states - n4 < 4 ? a.states - n4 : 4);
     const uint32_t bc0 = (uint32_t)group * a.states + (bcn ? n4 : 0);
     Raw<T, 2, ODD> nx[RPT], nd[RPT], nz[RPT];
@@ -239,7 +252,7 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
             const uint8_t* base = row_of(p, r, stride);
 #pragma unroll
             for (int k = 0; k < BCV; k++) {
-                int32_t row = bcrow + k * (256 / S);
+                int32_t row = bcrow + k * (256 / VS);
                 if (!WHOLE && row > most) row = most;
                 q[k].load(base, ((uint32_t)row * (uint32_t)stride + bc0) * SZ, bcn);
             }
@@ -271,47 +284,45 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
         }
 #pragma unroll
         for (int k = 0; k < BCV; k++) {
-            const int row = bcrow + k * (256 / S);
+            const int row = bcrow + k * (256 / VS);
             const bool out = tail && r + row >= row1;
             const auto values = [&](const Raw<T, 4, ODD>& q) {
                 float4 v = make_float4(q.get(0), q.get(1), q.get(2), q.get(3));
                 if (ODD) v = make_float4(bcn > 0 ? v.x : 0.0f, bcn > 1 ? v.y : 0.0f, bcn > 2 ? v.z : 0.0f, bcn > 3 ? v.w : 0.0f);
                 return out ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : v;
             };
-            sB[row][n4 / 4] = values(nB[k]);
-            if (MODE != SCAN_PIECE_STATE) sC[row][n4 / 4] = values(nC[k]);
+            *(float4*)&sB[row][n4] = values(nB[k]);
+            if (MODE != SCAN_PIECE_STATE) *(float4*)&sC[row][n4] = values(nC[k]);
         }
         __syncthreads();
         if (r + TT < row1) fetch(r + TT);
 
         // four rows at a time, the next two always on their way from LDS; rows past the end change nothing
         const int rows = row1 - r < TT ? row1 - r : TT;
-        Rows2 even, odd;
-        auto read = [&](Rows2& q, int t) {
+        Rows2<NS> even, odd;
+        auto read = [&](Rows2<NS>& q, int t) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
                 q.v[u] = dtx[t + u][ch];
-                q.b[u] = sB[t + u][s];
-                if (MODE != SCAN_PIECE_STATE) q.c[u] = sC[t + u][s];
+                __builtin_memcpy(q.b[u], __builtin_assume_aligned(&sB[t + u][NS * s], 4 * NS), 4 * NS);
+                if (MODE != SCAN_PIECE_STATE) __builtin_memcpy(q.c[u], __builtin_assume_aligned(&sC[t + u][NS * s], 4 * NS), 4 * NS);
             }
         };
         float p[4];
-        auto step = [&](const Rows2& q, int at) {
+        auto step = [&](const Rows2<NS>& q, int at) {
 #pragma unroll
             for (int u = 0; u < 2; u++) {
                 const float2 v = q.v[u];
-                const float bb[4] = {q.b[u].x, q.b[u].y, q.b[u].z, q.b[u].w};
                 if (MODE == SCAN_PIECE_STATE) total += v.x;
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    h[j] = fmaf(__builtin_amdgcn_exp2f(v.x * A[j]), h[j], v.y * bb[j]);
+                for (int j = 0; j < NS; j++) {
+                    h[j] = fmaf(__builtin_amdgcn_exp2f(v.x * A[j]), h[j], v.y * q.b[u][j]);
                     if (ODD) h[j] = j < nv ? h[j] : 0.0f;    // an infinite input must not reach a state that is not there
                 }
                 if (MODE != SCAN_PIECE_STATE) {
-                    const float cc[4] = {q.c[u].x, q.c[u].y, q.c[u].z, q.c[u].w};
-                    p[at + u] = cc[0] * h[0];
+                    p[at + u] = q.c[u][0] * h[0];
 #pragma unroll
-                    for (int j = 1; j < 4; j++) p[at + u] = fmaf(cc[j], h[j], p[at + u]);
+                    for (int j = 1; j < NS; j++) p[at + u] = fmaf(q.c[u][j], h[j], p[at + u]);
                 }
             }
         };
@@ -363,11 +374,11 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
     }
     if (ch >= cn) return;
     if (MODE == SCAN_PIECE_STATE) {
-        store_row<4>(a.ws_state + unit * plane + state_at, nv, h);
+        store_row<NS>(a.ws_state + unit * plane + state_at, nv, h);
         if (s == 0) a.ws_sum[(int64_t)unit * a.channels + d] = total;
     } else if (piece == pieces - 1) {
         const int32_t slot = a.state ? seq_slot(a.seq, a.seq.to, i) : -1;
-        if (slot >= 0) store_row<4>(a.state + slot * a.slot_stride + state_at, nv, h);
+        if (slot >= 0) store_row<NS>(a.state + slot * a.slot_stride + state_at, nv, h);
     }
 }
 
@@ -438,81 +449,130 @@ __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
     }
 }
 
-// Lanes per channel: 4 states each.
-static int lanes_per_channel(int states)
+// Lanes per channel, NS states each.
+static int lanes_per_channel(int states, int NS)
 {
     int s = 1;
-    while (4 * s < states) s *= 2;
+    while (NS * s < states) s *= 2;
     return s;
 }
 
 static bool is_step(const icv_sequences* seq) { return !seq->start && seq->tokens == seq->count; }
 
-// Rows per piece of a sequence, 0 where sequences stay whole.  Pieces cost a second pass over the rows that makes no outputs
-// (0.7 of the first), and fill a chip that whole sequences leave idle: 16384 rows of 2048 channels (32 workgroups) take 1724 us
-// whole, 255 in pieces of 256; 5 sequences of 2501 rows, 1000 channels, 64 states (320 workgroups) 105 whole, waiting for the longest, 77
-// in pieces; 24 of 12347 rows, 4096 channels (1536 workgroups) 290 whole, 400 in pieces.  Equal lengths wait for no one and stay whole
-// from 200 workgroups on (8 x 2048 rows, 256 workgroups: 222 both ways; 6 x 2048: 218 whole, 172 in pieces).  Pieces of less than 128 rows
-// cost more in launches than they save (200 rows, 128 workgroups: 28 whole, 41).
-static int32_t piece_rows(const icv_scan_params* p, const icv_sequences* seq, int S)
+// How a call is cut: lanes per channel, states per lane, rows per piece of a sequence (0: sequences stay whole).
+struct ScanPlan {
+    int S, NS;
+    int32_t rows;
+};
+
+// Fewer states per lane shorten the steps that follow one another, for some more instructions in all; pieces let the rows of a
+// sequence be worked on side by side, for a second pass over most of them that makes no outputs.  Both sides are modelled, in us, and
+// the fastest cut is taken: `chain`, a row's steps in a wavefront by itself, against `work`, all rows' instructions on a
+// chip that is full; whichever is longer, and something of the other when they are close.  The lengths in a ragged batch
+// are in device memory: the longest is taken for that of a batch of varied lengths.  Constants fitted to 30 calls of 1 to 200
+// sequences, 1000 to 32768 rows, 64 to 8192 channels, 8 to 64 states, each cut in 4 to 15 ways (MI355X): the cut taken
+// was 1.01 times as slow as the fastest, 1.45 at worst before states per lane were a choice.  16384 rows of 2048 channels: 1748 us whole with 4
+// states per lane, 840 with one, 258 in pieces of 512; 8 x 2048 rows: 222, 190 (two states), 212, in pieces 220; 24 ragged
+// ones of 12347 rows, 4096 channels: 241, 221, 276, in pieces 298; 2 x 512 rows, 512 channels: 60, 41, 31, in pieces 19.
+static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
 {
-    if (is_step(seq)) return 0;
-    const int cw = 256 / S, tt = 8 * S < 64 ? 8 * S : 64, per_group = p->channels / p->groups;
-    const int64_t wgs = (int64_t)p->groups * ((per_group + cw - 1) / cw) * seq->count;
+    ScanPlan best = {lanes_per_channel(p->states, 4), 4, 0};
+    if (is_step(seq)) return best;
+    const int32_t per_group = p->channels / p->groups;
     const bool equal = seq->count == 1 || (!seq->start && !seq->length);
-    const int64_t mean = seq->tokens / seq->count;
-    if (wgs >= (equal ? 200 : 512) || mean < (equal ? 320 : 128) || seq->tokens < 320) return 0;
-    const int64_t pieces = (2048 + wgs - 1) / wgs;
-    int64_t rows = (mean + pieces - 1) / pieces;
-    if (rows < 128) rows = 128;
-    return (int32_t)((rows + tt - 1) / tt * tt);
+    const double tokens = seq->tokens, mean = tokens / seq->count;
+    const double longest = equal ? mean : fmin(tokens, mean * (1 + 0.8 * log((double)seq->count)));
+    double least = 1e30;
+    for (int NS = 4; NS >= 1; NS /= 2) {
+        if (NS < 4 && (p->states <= 4 || p->states > 16 * NS)) continue;
+        const int S = lanes_per_channel(p->states, NS), cw = 256 / S, tt = 8 * S < 64 ? 8 * S : 64;
+        const bool odd = p->states != S * NS || per_group % 2 != 0;
+        const double channels = (double)p->groups * ((per_group + cw - 1) / cw) * cw;
+        const double work = tokens * channels * (1.6 + 0.16 * S * NS + 0.13 * S) * 1e-6 * (odd ? 1.3 : 1.0);
+        const double chain = (0.03 + 0.014 * NS + 0.09 / S) * (odd ? 1.4 : 1.0);
+        const auto both = [](double a, double b) {
+            const double more = fmax(a, b), less = fmin(a, b);
+            return more + 0.25 * less * (less / more) * (less / more);
+        };
+        for (int32_t rows = 0; rows <= 1024; rows = rows ? 2 * rows : 128) {
+            if (rows >= (equal ? mean : tokens)) break;
+            double us = 9 + both(longest * chain, work);
+            if (rows) {
+                const int32_t r = (rows + tt - 1) / tt * tt;
+                const double whole = seq->count / (tokens / r + 0.5 * seq->count);      // pieces that end a sequence: no first pass
+                const double steps = fmin(longest, r) * chain;
+                us = 12 + both(0.7 * steps, 0.55 * work * fmax(0.0, 1 - whole)) + 1.05 * both(steps, work) + longest / r / 8;
+            }
+            if (us < least) {
+                least = us;
+                best = {S, NS, (rows + tt - 1) / tt * tt};
+            }
+        }
+    }
+    return best;
 }
 
 static int64_t piece_count(const icv_sequences* seq, int32_t rows) { return (int64_t)seq->tokens / rows + seq->count; }
 
 template <typename T, int S>
-static int launch(const ScanArgs& a, bool step, int64_t pieces, hipStream_t s)
+static int launch_step(const ScanArgs& a, hipStream_t s)
 {
     constexpr int CW = 256 / S;
-    const bool odd = a.states != 4 * S || a.per_group % 2 != 0;
-    if (step) {
-        const int64_t tiles = (a.channels + CW - 1) / CW;
-        const int64_t wgs = tiles * a.seq.count;
-        const bool two = wgs >= 2048 && a.states == 4 * S;      // more than the chip holds at once
-        const int64_t n = two ? tiles * (((int64_t)a.seq.count + 1) / 2) : wgs;
-        if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-        if (a.states != 4 * S) k_scan_step<T, S, true, 1><<<(uint32_t)n, 256, 0, s>>>(a);
-        else if (two) k_scan_step<T, S, false, 2><<<(uint32_t)n, 256, 0, s>>>(a);
-        else k_scan_step<T, S, false, 1><<<(uint32_t)n, 256, 0, s>>>(a);
-        ICV_HIP_CHECK(hipGetLastError());
-        return ICV_OK;
-    }
-    const int64_t n = (int64_t)a.group_tiles * (a.channels / a.per_group) * (a.chunk ? pieces : a.seq.count);
+    const int64_t tiles = (a.channels + CW - 1) / CW, wgs = tiles * a.seq.count;
+    const bool two = wgs >= 2048 && a.states == 4 * S;      // more than the chip holds at once
+    const int64_t n = two ? tiles * (((int64_t)a.seq.count + 1) / 2) : wgs;
+    if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
+    if (a.states != 4 * S) k_scan_step<T, S, true, 1><<<(uint32_t)n, 256, 0, s>>>(a);
+    else if (two) k_scan_step<T, S, false, 2><<<(uint32_t)n, 256, 0, s>>>(a);
+    else k_scan_step<T, S, false, 1><<<(uint32_t)n, 256, 0, s>>>(a);
+    ICV_HIP_CHECK(hipGetLastError());
+    return ICV_OK;
+}
+
+template <typename T, int S, int NS>
+static int launch(const ScanArgs& a, hipStream_t s)
+{
+    const bool odd = a.states != NS * S || a.per_group % 2 != 0;
+    const int64_t n = (int64_t)a.group_tiles * (a.channels / a.per_group) * (a.chunk ? a.units : a.seq.count);
     if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
     if (!a.chunk) {
-        if (odd) k_scan<T, S, true, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
-        else k_scan<T, S, false, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
+        if (odd) k_scan<T, S, NS, true, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
+        else k_scan<T, S, NS, false, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
         ICV_HIP_CHECK(hipGetLastError());
         return ICV_OK;
     }
-    if (odd) k_scan<T, S, true, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
-    else k_scan<T, S, false, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
+    if (odd) k_scan<T, S, NS, true, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
+    else k_scan<T, S, NS, false, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
     ICV_HIP_CHECK(hipGetLastError());
-    if (odd) k_scan<T, S, true, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
-    else k_scan<T, S, false, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
+    if (odd) k_scan<T, S, NS, true, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
+    else k_scan<T, S, NS, false, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;
 }
 
 template <typename T>
-static int launch_lanes(const ScanArgs& a, int S, bool step, int64_t pieces, hipStream_t s)
+static int launch_plan(const ScanArgs& a, const ScanPlan& plan, bool step, hipStream_t s)
 {
-    switch (S) {
-        case 1: return launch<T, 1>(a, step, pieces, s);
-        case 2: return launch<T, 2>(a, step, pieces, s);
-        case 4: return launch<T, 4>(a, step, pieces, s);
-        case 8: return launch<T, 8>(a, step, pieces, s);
-        default: return launch<T, 16>(a, step, pieces, s);
+    if (step) {
+        switch (plan.S) {
+            case 1: return launch_step<T, 1>(a, s);
+            case 2: return launch_step<T, 2>(a, s);
+            case 4: return launch_step<T, 4>(a, s);
+            case 8: return launch_step<T, 8>(a, s);
+            default: return launch_step<T, 16>(a, s);
+        }
+    }
+    switch (plan.NS * 32 + plan.S) {
+        case 4 * 32 + 1: return launch<T, 1, 4>(a, s);
+        case 4 * 32 + 2: return launch<T, 2, 4>(a, s);
+        case 4 * 32 + 4: return launch<T, 4, 4>(a, s);
+        case 4 * 32 + 8: return launch<T, 8, 4>(a, s);
+        case 2 * 32 + 4: return launch<T, 4, 2>(a, s);
+        case 2 * 32 + 8: return launch<T, 8, 2>(a, s);
+        case 2 * 32 + 16: return launch<T, 16, 2>(a, s);
+        case 1 * 32 + 8: return launch<T, 8, 1>(a, s);
+        case 1 * 32 + 16: return launch<T, 16, 1>(a, s);
+        default: return launch<T, 16, 4>(a, s);
     }
 }
 
@@ -545,7 +605,7 @@ extern "C" size_t icv_selective_scan_workspace_bytes(const icv_scan_params* p, c
     using namespace icv;
     SeqArgs sa;
     if (check_scan(p, seq, &sa) != ICV_OK || seq->count == 0 || seq->tokens == 0) return 0;
-    const int32_t rows = piece_rows(p, seq, lanes_per_channel(p->states));
+    const int32_t rows = plan_scan(p, seq).rows;
     if (!rows) return 0;
     return (size_t)piece_count(seq, rows) * p->channels * (p->states + 1) * sizeof(float);
 }
@@ -580,16 +640,16 @@ extern "C" int icv_selective_scan(const icv_scan_params* p, const icv_sequences*
         return ICV_ERR_INVALID_ARG;
     a.slot_stride = p->state_slot_stride ? p->state_slot_stride : (int64_t)p->channels * p->states;
     a.channels = p->channels; a.states = p->states; a.per_group = p->channels / p->groups; a.softplus = p->softplus;
-    const int S = lanes_per_channel(p->states), cw = 256 / S;
+    const ScanPlan plan = plan_scan(p, seq);
+    const int cw = 256 / plan.S;
     a.group_tiles = (a.per_group + cw - 1) / cw;
     a.by_length = (seq->start || seq->length) && seq->count > 1 && seq->count <= 64;
-    a.chunk = piece_rows(p, seq, S);
+    a.chunk = plan.rows;
     const int64_t pieces = a.chunk ? piece_count(seq, a.chunk) : 0;
     if (a.chunk && (!workspace || misaligned(workspace, 16))) return ICV_ERR_INVALID_ARG;
     a.units = (int32_t)pieces;
     a.ws_state = (float*)workspace;
     a.ws_sum = a.ws_state + pieces * a.channels * a.states;
     hipStream_t s = (hipStream_t)stream;
-    return p->dtype == ICV_F32 ? launch_lanes<float>(a, S, is_step(seq), pieces, s)
-                               : launch_lanes<__bf16>(a, S, is_step(seq), pieces, s);
+    return p->dtype == ICV_F32 ? launch_plan<float>(a, plan, is_step(seq), s) : launch_plan<__bf16>(a, plan, is_step(seq), s);
 }
