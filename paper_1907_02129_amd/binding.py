@@ -457,7 +457,7 @@ def matmul_fp8(p, a, a_scales, b, b_scales, bias, output, stream=None):
           _matrix("a", a, M, K, p.a_row_stride or K, _CODES, dev), _vector("a_scales", a_scales, kb * M, f32, dev),
           _matrix("b", b, N, K, p.b_row_stride or K, _CODES, dev), _vector("b_scales", b_scales, kb * -(-N // 128), f32, dev),
           _vector("bias", bias, N, f32, dev),
-          _matrix("output", output, M, N, p.out_row_stride or N, torch.bfloat16 if p.out_type else f32, dev))
+          _matrix("output", output, M, N, p.out_row_stride or N, torch.bfloat16 if p.out_type & 255 else f32, dev))
 
 
 # ---------------------------------------------------------------- convenience: buffers for one problem

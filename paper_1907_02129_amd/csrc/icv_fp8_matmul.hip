@@ -407,6 +407,7 @@ static int launch_split(const MatmulArgs& g, hipStream_t s)
 // 1.05, the tiles of 32 x 64 whose 4 groups share the reduction 1.12 (64 rows, 8192 columns, 4096 deep: 11.5 us, 15.5 with 64 x 64).
 // Float outputs have no 256 x 256 tile: widened operands leave no room in the registers (5284 x 6015, 256 deep: 49.6 us, 38.3 with
 // 128 x 64).
+constexpr int64_t kMostTileStride = 1 << 23;       // the tile kernels keep a tile's offsets in 32 bits
 struct MatmulKernel {
     int32_t cols, rows, groups;
     double alone, busy, out;
@@ -418,10 +419,12 @@ static const MatmulKernel kKernels[2][KERNELS] = {
     {{256, 256, 1, 1e9, 1e9, 0.0}, {128, 128, 1, 1.14, 1.80, 1.03}, {128, 64, 1, 0.72, 0.85, 0.54}, {64, 64, 1, 0.48, 0.52, 0.22},
      {32, 64, 4, 0.93, 1.83, 0.11}, {16, 16, 8, 0.62, 0.67, 0.0}}};
 
-static int choose_kernel(const MatmulArgs& g, bool exact)
+// `hook`: a test hook, bits 8-11 of icv_matmul_params::out_type (icv.h says they must be 0; the library's own tests set them to run
+// every kernel on products small enough for a reference): 1 + the kernel.
+static int choose_kernel(const MatmulArgs& g, bool exact, int hook)
 {
-    // the tile kernels keep a tile's offsets in 32 bits
-    if (g.as >= (1 << 23) || g.bs >= (1 << 23)) return SPLIT;
+    if (hook) return hook - 1;
+    if (g.as >= kMostTileStride || g.bs >= kMostTileStride) return SPLIT;
     int best = SPLIT;
     double least = 1e30;
     for (int k = 0; k < KERNELS; k++) {
@@ -436,10 +439,10 @@ static int choose_kernel(const MatmulArgs& g, bool exact)
 }
 
 template <typename OUT>
-static int launch(const MatmulArgs& g, hipStream_t s)
+static int launch(const MatmulArgs& g, int hook, hipStream_t s)
 {
     constexpr bool EXACT = std::is_same<OUT, float>::value;
-    switch (choose_kernel(g, EXACT)) {
+    switch (choose_kernel(g, EXACT, hook)) {
         case TILE_256:
             if constexpr (!EXACT) return launch_tile<OUT, 256, 256, 2, 4, 1, true>(g, s);
         case TILE_128: return launch_tile<OUT, 128, 128, 2, 2, 1, false>(g, s);
@@ -459,7 +462,8 @@ extern "C" int icv_matmul_fp8(const icv_matmul_params* p, const void* a, const f
 {
     using namespace icv;
     if (!p || p->rows < 0 || p->cols < 1 || p->depth < 1 || p->depth > INT32_MAX - 127 || p->cols > INT32_MAX - 255) return ICV_ERR_INVALID_ARG;
-    if (p->out_type != ICV_OUT_ACC && p->out_type != ICV_OUT_BF16) return ICV_ERR_INVALID_ARG;
+    const int out_type = p->out_type & 255, hook = p->out_type >> 8;
+    if (p->out_type < 0 || (out_type != ICV_OUT_ACC && out_type != ICV_OUT_BF16)) return ICV_ERR_INVALID_ARG;
     const int32_t blocks = (p->depth + 127) / 128;
     for (int32_t r : {p->a_row_stride, p->b_row_stride})
         if (r && (r % 16 != 0 || r < (int64_t)blocks * 128)) return ICV_ERR_INVALID_ARG;
@@ -467,11 +471,14 @@ extern "C" int icv_matmul_fp8(const icv_matmul_params* p, const void* a, const f
     if (p->rows == 0) return ICV_OK;
     if (!a || !a_scales || !b || !b_scales || !out) return ICV_ERR_INVALID_ARG;
     const auto off = [](const void* q, uintptr_t bytes) { return ((uintptr_t)q & (bytes - 1)) != 0; };
-    if (off(a, 16) || off(b, 16) || off(a_scales, 4) || off(b_scales, 4) || off(bias, 4) || off(out, p->out_type == ICV_OUT_ACC ? 4 : 2))
+    if (off(a, 16) || off(b, 16) || off(a_scales, 4) || off(b_scales, 4) || off(bias, 4) || off(out, out_type == ICV_OUT_ACC ? 4 : 2))
         return ICV_ERR_INVALID_ARG;
     if (out == a || out == b) return ICV_ERR_INVALID_ARG;
     MatmulArgs g = {(const uint8_t*)a, (const uint8_t*)b, a_scales, b_scales, bias, out, p->rows, p->cols, blocks, (p->cols + 127) / 128,
                     p->a_row_stride ? p->a_row_stride : (int64_t)blocks * 128, p->b_row_stride ? p->b_row_stride : (int64_t)blocks * 128,
                     p->out_row_stride ? p->out_row_stride : p->cols};
-    return p->out_type == ICV_OUT_ACC ? launch<float>(g, (hipStream_t)stream) : launch<__bf16>(g, (hipStream_t)stream);
+    if (hook && (hook > KERNELS || (hook - 1 == TILE_256 && out_type == ICV_OUT_ACC) ||
+                 (hook - 1 != SPLIT && (g.as >= kMostTileStride || g.bs >= kMostTileStride))))
+        return ICV_ERR_UNSUPPORTED;
+    return out_type == ICV_OUT_ACC ? launch<float>(g, hook, (hipStream_t)stream) : launch<__bf16>(g, hook, (hipStream_t)stream);
 }

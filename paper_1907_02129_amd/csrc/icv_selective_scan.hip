@@ -465,6 +465,16 @@ struct ScanPlan {
     int32_t rows;
 };
 
+// Test hooks in icv_scan_params::softplus above its public value (icv.h says they must be 0; the library's own tests set them to run every
+// cut on calls small enough for a reference): bits 8-9 1: four states per lane, 2: two, 3: one; bits 10-15 rows per piece in 64s
+// (0: whole sequences).
+static int hook_states_per_lane(int hook) { return 8 >> (hook & 3); }
+static bool hook_fits(int hook, int states)
+{
+    const int NS = hook_states_per_lane(hook);
+    return (hook & 3) != 0 && hook < 256 && (NS == 4 || (states > 4 && states <= 16 * NS));
+}
+
 // Fewer states per lane shorten the steps that follow one another, for some more instructions in all; pieces let the rows of a
 // sequence be worked on side by side, for a second pass over most of them that makes no outputs.  Both sides are modelled, in us, and
 // the fastest cut is taken: `chain`, a row's steps in a wavefront by itself, against `work`, all rows' instructions on a
@@ -478,6 +488,10 @@ static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
 {
     ScanPlan best = {lanes_per_channel(p->states, 4), 4, 0};
     if (is_step(seq)) return best;
+    if (const int hook = p->softplus >> 8) {
+        const int NS = hook_states_per_lane(hook), S = lanes_per_channel(p->states, NS), tt = 8 * S < 64 ? 8 * S : 64;
+        return {S, NS, ((hook >> 2) * 64 + tt - 1) / tt * tt};
+    }
     const int32_t per_group = p->channels / p->groups;
     const bool equal = seq->count == 1 || (!seq->start && !seq->length);
     const double tokens = seq->tokens, mean = tokens / seq->count;
@@ -583,7 +597,8 @@ static int check_scan(const icv_scan_params* p, const icv_sequences* seq, SeqArg
 {
     if (!p || p->channels < 1 || p->states < 1 || p->groups < 1 || p->channels % p->groups != 0) return ICV_ERR_INVALID_ARG;
     if (p->states > 64) return ICV_ERR_UNSUPPORTED;
-    if (p->softplus != 0 && p->softplus != 1) return ICV_ERR_INVALID_ARG;
+    if (p->softplus < 0 || (p->softplus & 255) > 1) return ICV_ERR_INVALID_ARG;
+    if (p->softplus >> 8 && !hook_fits(p->softplus >> 8, p->states)) return ICV_ERR_UNSUPPORTED;
     if (p->dtype == ICV_U8I8) return ICV_ERR_UNSUPPORTED;
     if (p->dtype != ICV_F32 && p->dtype != ICV_BF16) return ICV_ERR_INVALID_ARG;
     for (int32_t r : {p->x_row_stride, p->dt_row_stride, p->z_row_stride, p->out_row_stride})
@@ -639,7 +654,7 @@ extern "C" int icv_selective_scan(const icv_scan_params* p, const icv_sequences*
         a.out == a.B || a.out == a.C)
         return ICV_ERR_INVALID_ARG;
     a.slot_stride = p->state_slot_stride ? p->state_slot_stride : (int64_t)p->channels * p->states;
-    a.channels = p->channels; a.states = p->states; a.per_group = p->channels / p->groups; a.softplus = p->softplus;
+    a.channels = p->channels; a.states = p->states; a.per_group = p->channels / p->groups; a.softplus = p->softplus & 255;
     const ScanPlan plan = plan_scan(p, seq);
     const int cw = 256 / plan.S;
     a.group_tiles = (a.per_group + cw - 1) / cw;

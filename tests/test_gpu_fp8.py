@@ -94,13 +94,17 @@ def wide_codes(c, pad):
     return full.cuda()[:, :c.shape[1]]
 
 
-def matmul_case(M, N, K, out, bias, seed, pad=0, far=False):
+KERNELS = {"256": 1, "128": 2, "128x64": 3, "64": 4, "32x64": 5, "split": 6}      # test hooks
+
+
+def matmul_case(M, N, K, out, bias, seed, pad=0, far=False, kernel=0):
     a, sa, b, sb, bs = operands(M, N, K, seed, far)
     kb = a.shape[1]
     t = TYPE[out]
     room = torch.full((M + 2, N + pad), 3.0, dtype=t, device="cuda")
     y = room[1:M + 1, :N]
     p = icv.make_matmul_params(M, N, K, out, kb + 16 * pad, kb + 32 * pad, N + pad)
+    p.out_type |= kernel << 8
     icv.matmul_fp8(p, wide_codes(a, 16 * pad), sa.cuda(), wide_codes(b, 32 * pad), sb.cuda(), bs.cuda() if bias else None, y)
     torch.cuda.synchronize()
     want, bound = ref.matmul(a, sa, b, sb, bs if bias else None, t)
@@ -121,16 +125,16 @@ def test_matmul_larger(M, N, K):
     matmul_case(M, N, K, "bf16", False, M + K)
 
 
-@pytest.mark.parametrize("M,N,K,out", [
-    # every kernel on sizes that are no multiple of its tile, the reduction of one block, of an odd number and of many
-    (3000, 5000, 128, "bf16"), (2900, 3100, 1100, "bf16"), (2177, 4100, 2400, "bf16"),     # 256 x 256
-    (1500, 3100, 900, "bf16"), (2900, 3100, 1100, "f32"), (3000, 4100, 129, "f32"),        # 128 x 128
-    (1100, 2050, 700, "bf16"), (1100, 2050, 700, "f32"),                                   # 128 x 64
-    (500, 2050, 384, "bf16"), (700, 1030, 600, "f32"),                                     # 64 x 64
-    (100, 2050, 3000, "bf16"), (70, 1030, 2200, "f32"), (64, 100, 500, "bf16"),            # 32 x 64 in four groups
-    (13, 1000, 8000, "bf16"), (3, 500, 512, "f32"), (1, 4099, 1920, "f32"),                # 16 x 16 in eight or four
-])
-def test_matmul_every_tile(M, N, K, out):
+@pytest.mark.parametrize("kernel,out", [(k, o) for k in KERNELS for o in ("bf16", "f32") if (k, o) != ("256", "f32")])
+def test_matmul_every_kernel(kernel, out):
+    """Every kernel on sizes that are no multiple of its tile, with reductions of one block, of a few and of many."""
+    for M, N, K in ((1, 1, 5), (300, 270, 128), (70, 300, 256), (257, 130, 1100), (129, 600, 700), (31, 65, 3000), (520, 513, 384)):
+        matmul_case(M, N, K, out, True, M + N + K, pad=M % 2, kernel=KERNELS[kernel])
+
+
+@pytest.mark.parametrize("M,N,K,out", [(3000, 5000, 128, "bf16"), (2900, 3100, 1100, "bf16"), (2900, 3100, 1100, "f32"),
+                                       (1100, 2050, 700, "bf16"), (500, 2050, 384, "bf16"), (100, 2050, 3000, "bf16"), (13, 1000, 8000, "bf16")])
+def test_matmul_the_kernels_own_sizes(M, N, K, out):
     matmul_case(M, N, K, out, True, M + N + K, pad=M % 2)
 
 

@@ -103,7 +103,8 @@ def test_causal_conv_batches(name, dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_causal_conv_taps(taps, dtype):
     for name in ("packed", "padded", "short_ones", "steps"):
-        conv_case(BATCHES[name], 24, taps, dtype, False, True, True, 1, taps)
+        for channels in (24, 23):
+            conv_case(BATCHES[name], channels, taps, dtype, False, True, True, 1, taps)
 
 
 @pytest.mark.parametrize("channels", [1, 7, 8, 9, 63, 130, 515, 2056])
@@ -113,7 +114,7 @@ def test_causal_conv_widths_and_alignments(channels, dtype):
     conv_case(BATCHES["one_long"], channels, 3, dtype, True, True, False, 0, channels)
 
 
-def scan_case(batch, channels, states, groups, dtype, softplus, extras, state, pad, seed, scale=1.0):
+def scan_case(batch, channels, states, groups, dtype, softplus, extras, state, pad, seed, scale=1.0, hook=0):
     g, t = gen(seed), TYPE[dtype]
     keep, n = batch.inside(), batch.tokens
 
@@ -135,6 +136,7 @@ def scan_case(batch, channels, states, groups, dtype, softplus, extras, state, p
     bc = groups * states
     p = icv.make_scan_params(channels, states, dtype, groups, softplus, channels + pad, channels + 2 * pad, bc + 3 * pad, bc + pad,
                              channels + pad, channels + 2 * pad, batch.slots if state else 0)
+    p.softplus |= hook << 8
     seq, std, outd = batch.seq(), st.cuda(), wide(out, 2 * pad)
     dev = lambda v: None if v is None else v.cuda()  # noqa: E731
     space = icv.selective_scan_workspace_bytes(p, seq)
@@ -163,6 +165,31 @@ def test_selective_scan_batches(name, dtype):
 def test_selective_scan_state_sizes(states, dtype):
     for name in ("packed", "steps"):
         scan_case(BATCHES[name], 21, states, 3, dtype, True, True, True, 1, states)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("per_lane,states", [(4, 4), (4, 3), (4, 8), (4, 6), (4, 16), (4, 12), (4, 32), (4, 29), (4, 64), (4, 47),
+                                             (2, 8), (2, 5), (2, 16), (2, 13), (2, 32), (2, 20), (1, 8), (1, 7), (1, 16), (1, 10)])
+def test_selective_scan_every_cut(per_lane, states, dtype):
+    """Every number of states per lane and lanes per channel, whole sequences and pieces of 64 rows (test hooks)."""
+    code = {4: 1, 2: 2, 1: 3}[per_lane]
+    for name in ("packed", "padded"):
+        for rows in (0, 1):
+            space = scan_case(BATCHES[name], 44, states, 2, dtype, True, True, True, 1, states, scale=0.1, hook=code | rows << 2)
+            assert (space > 0) == (rows > 0)
+    scan_case(BATCHES["one_long"], 21, states, 3, dtype, False, False, False, 0, states, scale=0.1, hook=code | 2 << 2)
+
+
+@pytest.mark.parametrize("states", [4, 8, 16, 32, 64])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_single_tokens_of_more_sequences_than_the_chip_holds(states, dtype):
+    """Two sequences to a workgroup, an odd number of them, some without rows, some without a slot."""
+    count, channels = 259, 8 * 64 if states == 16 else {4: 2048, 8: 1024, 32: 256, 64: 128}[states]
+    g = gen(states)
+    lengths = (torch.rand(count, generator=g) < 0.9).int().tolist()
+    batch = Batch(lengths, "step", source=[i if i % 5 else -1 for i in range(count)], target=[count + i if i % 7 else 10 ** 6 for i in range(count)],
+                  slots=2 * count)
+    scan_case(batch, channels, states, 2, dtype, True, True, True, 1, states)
 
 
 @pytest.mark.parametrize("channels,groups", [(1, 1), (2, 2), (63, 1), (65, 5), (130, 2), (264, 4), (515, 5)])

@@ -112,6 +112,8 @@ def test_scan_pointers_are_checked(lib):
     assert scan(lib, states=65) == UNSUPPORTED and scan(lib, dtype=icv.ICV_U8I8) == UNSUPPORTED
     for name in ("x", "dt", "b", "c", "z", "out"):
         assert scan(lib, **{name + "_row_stride": 1 << 24}) == UNSUPPORTED
+    for hook, states in ((4, 16), (2, 4), (2, 33), (3, 17), (256 + 1, 16)):              # test hooks that no kernel answers to
+        assert scan(lib, softplus=hook << 8, states=states) == UNSUPPORTED
     p = icv.make_scan_params(16, 16)
     assert lib.icv_selective_scan(p, seq(), None, None, None) == BAD
     assert lib.icv_selective_scan(None, seq(), icv.icv_scan_tensors(), None, None) == BAD
@@ -158,7 +160,8 @@ def test_quantisations_that_make_no_sense_are_refused(lib, kw):
 
 
 @pytest.mark.parametrize("kw", [dict(rows=-1), dict(cols=0), dict(depth=0), dict(depth=2 ** 31 - 1), dict(a_row_stride=368), dict(a_row_stride=392),
-                                dict(b_row_stride=383), dict(out_row_stride=19), dict(out_type=icv.ICV_OUT_U8), dict(out_type=9)])
+                                dict(b_row_stride=383), dict(out_row_stride=19), dict(out_type=icv.ICV_OUT_U8), dict(out_type=9),
+                                dict(out_type=-1)])
 def test_products_that_make_no_sense_are_refused(lib, kw):
     assert matmul(lib, **kw) == BAD
 
@@ -171,6 +174,9 @@ def test_pointers_of_the_8_bit_operators_are_checked(lib):
         assert matmul(lib, {name: None}) == BAD and matmul(lib, {name: ADDRESS + odd}) == BAD
     assert quantize(lib, {"codes": ADDRESS}) == BAD                                     # over their inputs
     assert matmul(lib, {"out": ADDRESS}) == BAD and matmul(lib, {"out": ADDRESS + 8192}) == BAD
+    for hook in (7, 15, 1 << 10):                                                       # test hooks that no kernel answers to
+        assert matmul(lib, out_type=icv.ICV_OUT_BF16 | hook << 8) == UNSUPPORTED
+    assert matmul(lib, out_type=icv.ICV_OUT_ACC | 1 << 8) == UNSUPPORTED
     assert matmul(lib, {"bias": ADDRESS + 1}) == BAD and matmul(lib, rows=0) == OK
     assert matmul(lib, {"out": ADDRESS + 2}, out_type=icv.ICV_OUT_ACC) == BAD
     assert lib.icv_quantize_fp8(None, ADDRESS, ADDRESS, ADDRESS, None) == BAD
