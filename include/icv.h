@@ -6,7 +6,8 @@
  * output pixel and kernel element, the input pixel row to read (section 2.3),
  * and an Indirect GEMM that accumulates output tiles over R*S*C by gathering
  * rows of A through that buffer (section 2.2, Listing 3), so that no im2col
- * matrix is ever written.
+ * matrix is ever written.  Beside it stand operators of layers along sequences
+ * and a matrix product in 8-bit floating point (their own sections below).
  *
  * Conventions that hold for every entry point
  *  - Tensors: input NHWC, output NHWC, filter [K][R][S][C] (Listing 1).
@@ -269,7 +270,7 @@ ICV_API int icv_conv2d_nhwc_im2col_static(const icv_conv_params* p, const void* 
  *            NULL: slot i
  *   to     : count entries: the slot that takes the state behind the sequence's last row; a value outside 0..slots-1:
  *            it is not kept.  NULL: slot i
- * Rows of no sequence are neither read nor written.  A sequence of no rows leaves every slot as it is.  Start values
+ * Rows of no sequence play no part, whatever they hold, and are not written.  A sequence of no rows leaves every slot as it is.  Start values
  * outside 0..tokens are taken as the nearer bound and never lead out of the tensors; where they decrease, which rows are computed is
  * undefined.  A slot may be continued by several sequences; a slot that a sequence writes must not be read or written
  * by another one of the same call (reading and writing the same slot by one sequence is the usual case).
