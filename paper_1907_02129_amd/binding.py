@@ -102,7 +102,7 @@ _lib = None
 
 def load_library(path: str | None = None):
     """Load libicv.so (built in-tree by `python -m paper_1907_02129_amd.build`)."""
-    global _lib
+    global _lib, _native
     if _lib is not None and path is None:
         return _lib
     path = path or LIB_PATH
@@ -149,7 +149,7 @@ def load_library(path: str | None = None):
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = res, args
-    _lib = lib
+    _lib, _native = lib, None          # _native calls the library that is loaded
     return lib
 
 
@@ -300,82 +300,68 @@ def conv2d_nhwc_im2col_static(p, input, packed_filter, output, stream=None):
 
 # ---------------------------------------------------------------- operators on sequences and in 8-bit floating point
 # These take views (a slice of a wider matrix is the usual input), so the tensors are checked against the problem's
-# description here: the library sees addresses only.  A small call's host time is these checks: each asks a tensor for no
-# more than it needs, and the messages are made where one fails.
-_TORCH = {ICV_F32: torch.float32, ICV_BF16: torch.bfloat16}
-_CODES = (torch.float8_e4m3fn, torch.uint8)
+# description: the library sees addresses only.  The checks and the call are icv_python.cpp's (ValueError for a tensor that
+# does not fit, TypeError for something else than a tensor), the stream and the device are chosen here.
+_native = None
 
 
-def _matrix(name, t, rows, cols, stride, dtype, device):
-    """Address of a [rows][cols] matrix whose rows lie `stride` elements apart."""
-    m, n = t.shape
-    a, b = t.stride()
-    if (t.dtype is not dtype and (dtype is not _CODES or t.dtype not in _CODES)) or t.get_device() != device or m < rows or n < cols or (
-            a != stride and rows > 1) or (b != 1 and cols > 1):
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}; {dtype}, at least {(rows, cols)}, strides "
-                         f"{(stride, 1)}, on GPU {device} expected")
-    return t.data_ptr()
+def _load_native():
+    global _native
+    if _native is None:
+        lib = load_library()
+        try:
+            from . import _icv_python as native
+        except ImportError as e:
+            raise RuntimeError(f"_icv_python.so: {e}; build it with `python -m paper_1907_02129_amd.build`") from e
+        address = lambda name: ctypes.cast(getattr(lib, name), ctypes.c_void_p).value  # noqa: E731
+        native.bind(*(address(n) for n in ("icv_causal_conv1d", "icv_selective_scan_workspace_bytes", "icv_selective_scan", "icv_quantize_fp8",
+                                           "icv_matmul_fp8")),
+                    icv_sequences, icv_causal_conv_params, icv_scan_params, icv_quantize_params, icv_matmul_params)
+        _native = native
+    return _native
 
 
-def _vector(name, t, n, dtype, device):
-    """Address of a contiguous tensor of at least n elements; None for none."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.get_device() != device or t.numel() < n or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous tensor of {dtype} with at least {n} elements on GPU {device} expected")
-    return t.data_ptr()
-
-
-def _slots(name, t, slots, per_slot, slot_stride, dtype, device):
-    """Address of at least `slots` state slots of per_slot elements, each contiguous, slot_stride apart; None for none."""
-    if t is None or per_slot == 0:
-        return None
-    shape = t.shape
-    if t.dtype is not dtype or t.get_device() != device or len(shape) < 2 or shape[0] < slots or t.numel() != shape[0] * per_slot or (
-            slots > 1 and t.stride(0) != slot_stride) or not (t.is_contiguous() or (slots > 0 and t[0].is_contiguous())):
-        raise ValueError(f"{name}: {slots} slots of {per_slot} elements of {dtype}, {slot_stride} apart, on GPU {device} expected")
-    return t.data_ptr()
-
-
-def _on_gpu(t) -> int:
-    device = t.get_device()
+def _call(name, first, stream, *args):
+    """The operator on the first tensor's device: on the given stream, which must be that device's, or its current one."""
+    device = first.get_device()
     if device < 0:
         raise ValueError("icv takes device tensors")
-    return device
-
-
-def _call(where, fn, device, stream, *args):
-    """fn(*args, stream) on the tensors' device: the given stream, which must be that device's, or its current one."""
     if stream is None:
         raw = torch._C._cuda_getCurrentRawStream(device)
     elif stream.device_index != device:
         raise ValueError("the stream is another device's")
     else:
         raw = stream.cuda_stream
+    fn = getattr(_native or _load_native(), name)
     if device == torch._C._cuda_getDevice():
-        status = fn(*args, raw)
+        status = fn(device, raw, *args)
     else:
         with torch.cuda.device(device):
-            status = fn(*args, raw)
+            status = fn(device, raw, *args)
     if status != ICV_OK:
-        raise IcvError(status, where)
+        raise IcvError(status, "icv_" + name)
+
+
+def _indices(name, t, n, device):
+    """Address of a contiguous int32 tensor of at least n elements; None for none."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.get_device() != device or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous int32 tensor of at least {n} elements, all such on one GPU, expected")
+    return t.data_ptr()
 
 
 def make_sequences(count, tokens, start=None, length=None, from_slot=None, to_slot=None) -> icv_sequences:
     """icv_sequences; the arrays are int32 device tensors, kept alive by the result.  `start` has count + 1 entries, the
     others count; what they hold is read when the kernels run."""
     arrays = tuple(t for t in (start, length, from_slot, to_slot) if t is not None)
-    device = _on_gpu(arrays[0]) if arrays else -1
-    i32 = torch.int32
-    s = icv_sequences(count, tokens, _vector("start", start, count + 1, i32, device), _vector("length", length, count, i32, device),
-                      _vector("from_slot", from_slot, count, i32, device), _vector("to_slot", to_slot, count, i32, device))
+    device = arrays[0].get_device() if arrays else -1
+    if arrays and device < 0:
+        raise ValueError("icv takes device tensors")
+    s = icv_sequences(count, tokens, _indices("start", start, count + 1, device), _indices("length", length, count, device),
+                      _indices("from_slot", from_slot, count, device), _indices("to_slot", to_slot, count, device))
     s.arrays, s.device = arrays, device
     return s
-
-
-def _same_device(seq, device):
-    if seq.device != device and seq.device >= 0:
-        raise ValueError("icv takes tensors of one device")
 
 
 def make_causal_conv_params(channels, taps, dtype="bf16", silu=True, in_row_stride=0, out_row_stride=0, state_slots=0,
@@ -387,13 +373,7 @@ def make_causal_conv_params(channels, taps, dtype="bf16", silu=True, in_row_stri
 def causal_conv1d(p, seq, input, filter, bias, state, output, stream=None):
     """Short causal convolution (icv_causal_conv1d): input and output [tokens, channels], filter [channels, taps], bias
     [channels] or None, state [slots, taps - 1, channels] (read and written) or None."""
-    t, n, D, W, dev = _TORCH.get(p.dtype), seq.tokens, p.channels, p.taps, _on_gpu(input)
-    _same_device(seq, dev)
-    per_slot = (W - 1) * D
-    _call("icv_causal_conv1d", (_lib or load_library()).icv_causal_conv1d, dev, stream, p, seq,
-          _matrix("input", input, n, D, p.in_row_stride or D, t, dev), _vector("filter", filter, D * W, t, dev),
-          _vector("bias", bias, D, torch.float32, dev), _slots("state", state, p.state_slots, per_slot, p.state_slot_stride or per_slot, t, dev),
-          _matrix("output", output, n, D, p.out_row_stride or D, t, dev))
+    _call("causal_conv1d", input, stream, p, seq, input, filter, bias, state, output)
 
 
 def make_scan_params(channels, states, dtype="bf16", groups=1, softplus=True, x_row_stride=0, dt_row_stride=0, b_row_stride=0,
@@ -410,21 +390,7 @@ def selective_scan(p, seq, x, dt, A, B, C, D, z, dt_bias, state, output, workspa
     """Selective scan (icv_selective_scan): x, dt, z, output [tokens, channels], B, C [tokens, groups * states], A [channels,
     states], D, dt_bias [channels]; D, z, dt_bias and state [slots, channels, states] (read and written) may be None.  `workspace`: a device tensor of
     selective_scan_workspace_bytes() bytes at least, which may be None where that is 0."""
-    t, n, ch, bc, f32, dev = _TORCH.get(p.dtype), seq.tokens, p.channels, p.groups * p.states, torch.float32, _on_gpu(x)
-    _same_device(seq, dev)
-    lib = _lib or load_library()
-    need = lib.icv_selective_scan_workspace_bytes(p, seq)
-    if need and (workspace is None or workspace.get_device() != dev or not workspace.is_contiguous()
-                 or workspace.numel() * workspace.element_size() < need):
-        raise ValueError(f"workspace: a contiguous tensor of at least {need} bytes on GPU {dev} expected")
-    tensors = icv_scan_tensors(
-        _matrix("x", x, n, ch, p.x_row_stride or ch, t, dev), _matrix("dt", dt, n, ch, p.dt_row_stride or ch, t, dev),
-        _vector("A", A, ch * p.states, f32, dev), _matrix("B", B, n, bc, p.b_row_stride or bc, t, dev),
-        _matrix("C", C, n, bc, p.c_row_stride or bc, t, dev), _vector("D", D, ch, f32, dev),
-        None if z is None else _matrix("z", z, n, ch, p.z_row_stride or ch, t, dev), _vector("dt_bias", dt_bias, ch, f32, dev),
-        _slots("state", state, p.state_slots, ch * p.states, p.state_slot_stride or ch * p.states, f32, dev),
-        _matrix("output", output, n, ch, p.out_row_stride or ch, t, dev))
-    _call("icv_selective_scan", lib.icv_selective_scan, dev, stream, p, seq, tensors, workspace.data_ptr() if need else None)
+    _call("selective_scan", x, stream, p, seq, x, dt, A, B, C, D, z, dt_bias, state, output, workspace)
 
 
 def make_quantize_params(rows, depth, dtype="bf16", block_rows=1, in_row_stride=0, code_row_stride=0) -> icv_quantize_params:
@@ -434,12 +400,7 @@ def make_quantize_params(rows, depth, dtype="bf16", block_rows=1, in_row_stride=
 def quantize_fp8(p, input, codes, scales, stream=None):
     """Quantisation into e4m3 (icv_quantize_fp8): input [rows, depth], codes [rows, depth up to a multiple of 128] of
     float8_e4m3fn or uint8, scales [blocks of 128 columns, blocks of rows]."""
-    M, K, br, dev = p.rows, p.depth, max(1, p.block_rows), _on_gpu(input)
-    kb = -(-K // 128)
-    _call("icv_quantize_fp8", (_lib or load_library()).icv_quantize_fp8, dev, stream, p,
-          _matrix("input", input, M, K, p.in_row_stride or K, _TORCH.get(p.dtype), dev),
-          _matrix("codes", codes, M, 128 * kb, p.code_row_stride or 128 * kb, _CODES, dev),
-          _vector("scales", scales, kb * -(-M // br), torch.float32, dev))
+    _call("quantize_fp8", input, stream, p, input, codes, scales)
 
 
 def make_matmul_params(rows, cols, depth, out="bf16", a_row_stride=0, b_row_stride=0, out_row_stride=0) -> icv_matmul_params:
@@ -450,14 +411,7 @@ def make_matmul_params(rows, cols, depth, out="bf16", a_row_stride=0, b_row_stri
 def matmul_fp8(p, a, a_scales, b, b_scales, bias, output, stream=None):
     """output = a @ b.T + bias with e4m3 operands (icv_matmul_fp8): a [rows, depth up to a multiple of 128] and b [cols, the
     same] of float8_e4m3fn or uint8 with their scales from quantize_fp8 (block_rows 1 and 128), bias [cols] or None."""
-    M, N, f32, dev = p.rows, p.cols, torch.float32, _on_gpu(a)
-    kb = -(-p.depth // 128)
-    K = 128 * kb
-    _call("icv_matmul_fp8", (_lib or load_library()).icv_matmul_fp8, dev, stream, p,
-          _matrix("a", a, M, K, p.a_row_stride or K, _CODES, dev), _vector("a_scales", a_scales, kb * M, f32, dev),
-          _matrix("b", b, N, K, p.b_row_stride or K, _CODES, dev), _vector("b_scales", b_scales, kb * -(-N // 128), f32, dev),
-          _vector("bias", bias, N, f32, dev),
-          _matrix("output", output, M, N, p.out_row_stride or N, torch.bfloat16 if p.out_type & 255 else f32, dev))
+    _call("matmul_fp8", a, stream, p, a, a_scales, b, b_scales, bias, output)
 
 
 # ---------------------------------------------------------------- convenience: buffers for one problem

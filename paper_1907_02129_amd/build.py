@@ -3,7 +3,8 @@
     python -m paper_1907_02129_amd.build
 
 Every .hip file under csrc/ is compiled to an object (in parallel) and linked into
-paper_1907_02129_amd/libicv.so.  hipcc cross-compiles without a GPU present.
+paper_1907_02129_amd/libicv.so.  hipcc cross-compiles without a GPU present.  The host compiler builds
+icv_python.cpp, the argument checks of the operators that take torch tensors, into _icv_python.so beside it.
 """
 from __future__ import annotations
 
@@ -12,12 +13,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libicv.so")
+PYTHON_MODULE = os.path.join(PKG, "_icv_python.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -47,12 +50,34 @@ def _compile(src: str, verbose: bool, incremental: bool = False) -> str:
     return obj
 
 
+def build_python_module(verbose: bool = False, incremental: bool = False) -> str:
+    import torch                                  # its headers and libraries; the module runs in a process that has torch loaded
+    src, at = os.path.join(CSRC, "icv_python.cpp"), os.path.dirname(os.path.abspath(torch.__file__))
+    deps = [src, os.path.join(ROOT, "include", "icv.h")]
+    if incremental and os.path.exists(PYTHON_MODULE) and all(os.path.getmtime(d) <= os.path.getmtime(PYTHON_MODULE) for d in deps):
+        return PYTHON_MODULE
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-isystem", os.path.join(at, "include"), "-isystem", os.path.join(at, "include", "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], src, "-o", PYTHON_MODULE, "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed on {src}:\n{r.stdout}")
+    if r.stdout.strip() and verbose:
+        print(r.stdout)
+    return PYTHON_MODULE
+
+
 def build(verbose: bool = False, jobs: int = 8, incremental: bool = False) -> str:
     """Compile every source (or, with `incremental`, those newer than their object) and link the library."""
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
-    with cf.ThreadPoolExecutor(max_workers=min(jobs, len(srcs))) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(jobs, len(srcs) + 1)) as ex:
+        module = ex.submit(build_python_module, verbose, incremental)
         objs = list(ex.map(lambda s: _compile(s, verbose, incremental), srcs))
+        module.result()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     if verbose:
         print(" ".join(cmd), flush=True)

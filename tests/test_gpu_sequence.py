@@ -438,3 +438,45 @@ def test_calls_on_a_stream_of_their_own():
         torch.cuda.synchronize()
         results.append((u, y))
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_the_binding_refuses_what_does_not_fit_the_description():
+    """Types, sizes, strides, state slots and workspaces: each wrong one is refused before the launch, and nothing is written."""
+    n, ch, N, W = 6, 16, 8, 4
+    t = lambda *shape, dtype=torch.bfloat16: torch.full(shape, 3.0, dtype=dtype, device="cuda")  # noqa: E731
+    x, f, y = t(n, ch), t(ch, W), t(n, ch)
+    st, p, seq = t(2, W - 1, ch), icv.make_causal_conv_params(ch, W, state_slots=2), icv.make_sequences(2, n)
+    bias = t(ch, dtype=torch.float32)
+    good = dict(input=x, filter=f, bias=bias, state=st, output=y)
+    for name, bad in (("input", t(n, ch, dtype=torch.float32)), ("input", t(n - 1, ch)), ("input", t(n, ch - 1)), ("input", t(n, 2 * ch)[:, :ch]),
+                      ("input", t(ch, n).t()), ("input", t(n, 1, ch)), ("input", x.cpu()), ("filter", t(ch, W - 1)), ("filter", t(W, ch).t()),
+                      ("filter", f.float()), ("bias", bias[:-1]), ("bias", bias.bfloat16()), ("state", t(1, W - 1, ch)), ("state", t(2, W, ch)),
+                      ("state", t(2, W - 1, 2 * ch)[:, :, :ch]), ("state", st.float()), ("output", t(n, 2 * ch)[:, ::2]), ("output", y.half())):
+        with pytest.raises(ValueError, match=name if bad.is_cuda or name != "input" else "device"):
+            icv.causal_conv1d(p, seq, *{**good, name: bad}.values())
+    assert (y == 3).all() and (st == 3).all()
+    with pytest.raises(icv.IcvError) as e:
+        icv.causal_conv1d(p, seq, x, f, bias, st, x)
+    assert e.value.status == icv.ICV_ERR_INVALID_ARG
+
+    p, seq = icv.make_scan_params(ch, N, state_slots=1), icv.make_sequences(1, 4000)
+    x, B, A, y = t(4000, ch), t(4000, N), t(ch, N, dtype=torch.float32), t(4000, ch)
+    need = icv.selective_scan_workspace_bytes(p, seq)
+    assert need > 0
+    for bad in (None, torch.empty(need - 1, dtype=torch.uint8, device="cuda"), torch.empty(need, dtype=torch.uint8),
+                torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            icv.selective_scan(p, seq, x, x, A, B, B, None, None, None, None, y, bad)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    for k, bad in ((2, A.bfloat16()), (3, B[:, :-1]), (4, t(4000, 2 * N)[:, :N]), (5, t(ch - 1, dtype=torch.float32)), (6, t(3999, ch)),
+                   (7, t(ch)), (8, t(1, ch, N)), (9, y.float())):
+        args = [x, x, A, B, B, None, None, None, None, y]
+        args[k] = bad
+        with pytest.raises(ValueError):
+            icv.selective_scan(p, seq, *args, ws)
+    with pytest.raises(ValueError):
+        icv.make_sequences(2, 8, start=ints([0, 8]))
+    with pytest.raises(ValueError):
+        icv.make_sequences(2, 8, length=torch.tensor([1, 2], device="cuda"))
+    torch.cuda.synchronize()
+    assert (y == 3).all()

@@ -191,3 +191,30 @@ def test_the_binding_refuses_host_tensors():
         icv.make_sequences(1, 4, start=torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError):
         icv.quantize_fp8(icv.make_quantize_params(4, 16), x, x, x)
+
+
+def test_the_checks_name_what_is_wrong():
+    """The native checks themselves, on host tensors, which they refuse for that at the latest: nothing is launched."""
+    native = icv._load_native()
+    x = torch.zeros(4, 16, dtype=torch.bfloat16)
+    p, s = icv.make_causal_conv_params(16, 4), seq(1, 4)
+    with pytest.raises(ValueError, match="input: a BFloat16 matrix of at least 4 x 16, strides .16, 1., on GPU 0 expected"):
+        native.causal_conv1d(0, 0, p, s, x, x, None, None, x)
+    with pytest.raises(TypeError, match="input: a tensor expected"):
+        native.causal_conv1d(0, 0, p, s, [1], x, None, None, x)
+    with pytest.raises(TypeError, match="icv_causal_conv_params"):
+        native.causal_conv1d(0, 0, s, s, x, x, None, None, x)
+    with pytest.raises(TypeError, match="icv_sequences"):
+        native.causal_conv1d(0, 0, p, p, x, x, None, None, x)
+    with pytest.raises(TypeError, match="9 arguments"):
+        native.causal_conv1d(0, 0, p, s, x)
+    with pytest.raises(ValueError, match="input: a BFloat16 matrix of at least 4 x 16"):
+        native.quantize_fp8(0, 0, icv.make_quantize_params(4, 16), x, x, x)
+    with pytest.raises(ValueError, match="a: a Byte matrix of at least 4 x 128"):
+        native.matmul_fp8(0, 0, icv.make_matmul_params(4, 16, 16), x, x, x, x, None, x)
+    with pytest.raises(ValueError, match="x: a Float matrix"):
+        native.selective_scan(0, 0, icv.make_scan_params(16, 16, "f32"), s, *[x] * 10, None)
+    other = seq(1, 4)
+    other.device = 1
+    with pytest.raises(ValueError, match="one device"):
+        native.causal_conv1d(0, 0, p, other, x, x, None, None, x)
