@@ -4,6 +4,10 @@
 // products run on the tensor cores, one 16 x 16 x 128 instruction per block; a block's sum is scaled and added to the
 // float accumulator on the vector ALU, one multiply-add per output and block (the two scales' product is the same for
 // the 4 outputs that a lane holds, which are neighbouring columns of one row).
+//
+// 12288 x 8192, 4096 deep to bfloat16: 390 us, 2.1 PFLOP/s (the vendor's product without block scales: 346; with operands of zeros 351,
+// the difference being power); to float 890.  8 x 4096, 2048 deep: 4.8 us, a launch; 8 x 4096, 8192 deep 10.6, 3.2 TB/s of filter;
+// 64 x 8192, 4096 deep 11.5; 1024 x 4096, 4096 deep 26, 1.3 PFLOP/s.
 #include "icv_mfma_common.h"
 #include <cmath>
 

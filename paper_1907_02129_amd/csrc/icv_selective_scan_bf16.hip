@@ -1,0 +1,8 @@
+// The scan's kernels (icv_selective_scan_kernel.h) for rows of bfloat16; its own translation unit for the build's parallelism.
+#include "icv_selective_scan_kernel.h"
+
+namespace icv {
+
+int launch_scan_bf16(const ScanArgs& a, const ScanPlan& plan, bool step, hipStream_t s) { return launch_scan<__bf16>(a, plan, step, s); }
+
+}  // namespace icv
