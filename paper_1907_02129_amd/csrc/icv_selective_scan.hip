@@ -31,9 +31,9 @@ static bool hook_fits(int hook, int states)
 // chip that is full; whichever is longer, and something of the other when they are close.  The lengths in a ragged batch
 // are in device memory: the longest is taken for that of a batch of varied lengths.  Constants fitted to 30 calls of 1 to 200
 // sequences, 1000 to 32768 rows, 64 to 8192 channels, 8 to 64 states, each cut in 4 to 15 ways (MI355X): the cut taken
-// was 1.01 times as slow as the fastest, 1.45 at worst before states per lane were a choice.  16384 rows of 2048 channels: 1748 us whole with 4
-// states per lane, 840 with one, 258 in pieces of 512; 8 x 2048 rows: 222, 190 (two states), 212, in pieces 220; 24 ragged
-// ones of 12347 rows, 4096 channels: 241, 221, 276, in pieces 298; 2 x 512 rows, 512 channels: 60, 41, 31, in pieces 19.
+// took 1.01 times as long as the fastest.  16384 rows of 2048 channels: 1743 us whole with 4 states per lane, 733 with one, 258
+// in pieces of 512; 8 x 2048 rows: 221, 182 (two states), 210, in pieces 220; 24 ragged ones of 12347 rows, 4096 channels: 234, 222,
+// 292, in pieces 298; 2 x 512 rows, 512 channels: 58, 36, 26, in pieces 17.
 static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
 {
     ScanPlan best = {lanes_per_channel(p->states, 4), 4, 0};
@@ -45,27 +45,27 @@ static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
     const int32_t per_group = p->channels / p->groups;
     const bool equal = seq->count == 1 || (!seq->start && !seq->length);
     const double tokens = seq->tokens, mean = tokens / seq->count;
-    const double longest = equal ? mean : fmin(tokens, mean * (1 + 0.8 * log((double)seq->count)));
+    const double longest = equal ? mean : fmin(tokens, mean * (1 + 1.1 * log((double)seq->count)));
     double least = 1e30;
     for (int NS = 4; NS >= 1; NS /= 2) {
         if (NS < 4 && (p->states <= 4 || p->states > 16 * NS)) continue;
         const int S = lanes_per_channel(p->states, NS), cw = 256 / S, tt = 8 * S < 64 ? 8 * S : 64;
         const bool odd = p->states != S * NS || per_group % 2 != 0;
         const double channels = (double)p->groups * ((per_group + cw - 1) / cw) * cw;
-        const double work = tokens * channels * (1.6 + 0.16 * S * NS + 0.13 * S) * 1e-6 * (odd ? 1.3 : 1.0);
-        const double chain = (0.03 + 0.014 * NS + 0.09 / S) * (odd ? 1.4 : 1.0);
+        const double work = tokens * channels * (1.55 + 0.178 * S * NS + 0.104 * S) * 1e-6 * (odd ? 1.3 : 1.0);
+        const double chain = (0.022 + 0.0146 * NS + 0.0745 / S) * (odd ? 1.4 : 1.0);
         const auto both = [](double a, double b) {
             const double more = fmax(a, b), less = fmin(a, b);
             return more + 0.25 * less * (less / more) * (less / more);
         };
         for (int32_t rows = 0; rows <= 1024; rows = rows ? 2 * rows : 128) {
             if (rows >= (equal ? mean : tokens)) break;
-            double us = 9 + both(longest * chain, work);
+            double us = 6.6 + both(longest * chain, work);
             if (rows) {
                 const int32_t r = (rows + tt - 1) / tt * tt;
                 const double whole = seq->count / (tokens / r + 0.5 * seq->count);      // pieces that end a sequence: no first pass
                 const double steps = fmin(longest, r) * chain;
-                us = 12 + both(0.7 * steps, 0.55 * work * fmax(0.0, 1 - whole)) + 1.05 * both(steps, work) + longest / r / 8;
+                us = 8.4 + both(0.7 * steps, 0.3 * work * fmax(0.0, 1 - whole)) + 1.23 * both(steps, work) + longest / r / 8;
             }
             if (us < least) {
                 least = us;

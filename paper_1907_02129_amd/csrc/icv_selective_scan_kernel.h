@@ -89,11 +89,11 @@ __device__ inline int32_t nth_longest(const SeqArgs& q, int32_t n, int lane)
     return __builtin_ctzll(__ballot(lane < q.count && rank == n));
 }
 
-// Two rows' values of a lane's channel and NS states.
-template <int NS>
-struct Rows2 {
-    float2 v[2];
-    float b[2][NS], c[2][NS];
+// R rows' values of a lane's channel and NS states.
+template <int NS, int R>
+struct Rows {
+    float2 v[R];
+    float b[R][NS], c[R][NS];
 };
 
 template <typename T, int S, int NS, bool ODD, int MODE>
@@ -285,21 +285,24 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
         __syncthreads();
         if (r + TT < row1) fetch(r + TT);
 
-        // four rows at a time, the next two always on their way from LDS; rows past the end change nothing
+        // Four rows at a time, the next AHEAD always on their way from LDS, which takes longer than two rows of one or two states (16384
+        // rows in one wavefront's steps: 843 -> 733 us with one, 1147 -> 1013 with two; with four states there are no registers for it, and
+        // two rows take long enough); the sums over the lanes are then taken while the next four are stepped through.  Rows past
+        // the end change nothing.
+        constexpr int AHEAD = NS == 4 ? 2 : 4;
         const int rows = row1 - r < TT ? row1 - r : TT;
-        Rows2<NS> even, odd;
-        auto read = [&](Rows2<NS>& q, int t) {
+        Rows<NS, AHEAD> even, odd;
+        auto read = [&](Rows<NS, AHEAD>& q, int t) {
 #pragma unroll
-            for (int u = 0; u < 2; u++) {
+            for (int u = 0; u < AHEAD; u++) {
                 q.v[u] = dtx[t + u][ch];
                 __builtin_memcpy(q.b[u], __builtin_assume_aligned(&sB[t + u][NS * s], 4 * NS), 4 * NS);
                 if (MODE != SCAN_PIECE_STATE) __builtin_memcpy(q.c[u], __builtin_assume_aligned(&sC[t + u][NS * s], 4 * NS), 4 * NS);
             }
         };
-        float p[4];
-        auto step = [&](const Rows2<NS>& q, int at) {
+        auto step = [&](const Rows<NS, AHEAD>& q, float* p) {
 #pragma unroll
-            for (int u = 0; u < 2; u++) {
+            for (int u = 0; u < AHEAD; u++) {
                 const float2 v = q.v[u];
                 if (MODE == SCAN_PIECE_STATE) total += v.x;
 #pragma unroll
@@ -308,32 +311,49 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
                     if (ODD) h[j] = j < nv ? h[j] : 0.0f;    // an infinite input must not reach a state that is not there
                 }
                 if (MODE != SCAN_PIECE_STATE) {
-                    p[at + u] = q.c[u][0] * h[0];
+                    p[u] = q.c[u][0] * h[0];
 #pragma unroll
-                    for (int j = 1; j < NS; j++) p[at + u] = fmaf(q.c[u][j], h[j], p[at + u]);
+                    for (int j = 1; j < NS; j++) p[u] = fmaf(q.c[u][j], h[j], p[u]);
                 }
             }
         };
-        read(even, 0);
-        for (int t = 0; t < rows; t += 4) {
-            read(odd, t + 2);
-            __builtin_amdgcn_sched_barrier(0);
-            step(even, 0);
-            read(even, t + 4 < TT ? t + 4 : 0);
-            __builtin_amdgcn_sched_barrier(0);
-            step(odd, 2);
-            if (MODE != SCAN_PIECE_STATE) {
-                float y[4];
-                reduce_rows<S>(p, s, y);
-                if constexpr (S >= 4) {
-                    if (s < 4) dtx[t + s][ch].x = y[0];
-                } else if constexpr (S == 2) {
-                    dtx[t + s][ch].x = y[0];
-                    dtx[t + 2 + s][ch].x = y[1];
-                } else {
+        auto finish = [&](const float (&p)[4], int t) {
+            if (MODE == SCAN_PIECE_STATE) return;
+            float y[4];
+            reduce_rows<S>(p, s, y);
+            if constexpr (S >= 4) {
+                if (s < 4) dtx[t + s][ch].x = y[0];
+            } else if constexpr (S == 2) {
+                dtx[t + s][ch].x = y[0];
+                dtx[t + 2 + s][ch].x = y[1];
+            } else {
 #pragma unroll
-                    for (int u = 0; u < 4; u++) dtx[t + u][ch].x = y[u];
-                }
+                for (int u = 0; u < 4; u++) dtx[t + u][ch].x = y[u];
+            }
+        };
+        read(even, 0);
+        float p[4], was[4];
+        if constexpr (AHEAD == 4) {
+            for (int t = 0; t < rows; t += 8) {
+                read(odd, t + 4);
+                __builtin_amdgcn_sched_barrier(0);
+                step(even, p);
+                if (t > 0) finish(was, t - 4);
+                read(even, t + 8 < TT ? t + 8 : 0);
+                __builtin_amdgcn_sched_barrier(0);
+                step(odd, was);
+                finish(p, t);
+            }
+            finish(was, (rows - 1) / 8 * 8 + 4);
+        } else {
+            for (int t = 0; t < rows; t += 4) {
+                read(odd, t + 2);
+                __builtin_amdgcn_sched_barrier(0);
+                step(even, p);
+                read(even, t + 4 < TT ? t + 4 : 0);
+                __builtin_amdgcn_sched_barrier(0);
+                step(odd, p + 2);
+                finish(p, t);
             }
         }
         __syncthreads();
