@@ -26,14 +26,15 @@ static bool hook_fits(int hook, int states)
 }
 
 // Fewer states per lane shorten the steps that follow one another, for some more instructions in all; pieces let the rows of a
-// sequence be worked on side by side, for a second pass over most of them that makes no outputs.  Both sides are modelled, in us, and
-// the fastest cut is taken: `chain`, a row's steps in a wavefront by itself, against `work`, all rows' instructions on a
-// chip that is full; whichever is longer, and something of the other when they are close.  The lengths in a ragged batch
-// are in device memory: the longest is taken for that of a batch of varied lengths.  Constants fitted to 30 calls of 1 to 200
-// sequences, 1000 to 32768 rows, 64 to 8192 channels, 8 to 64 states, each cut in 4 to 15 ways (MI355X): the cut taken
-// took 1.01 times as long as the fastest.  16384 rows of 2048 channels: 1743 us whole with 4 states per lane, 733 with one, 258
-// in pieces of 512; 8 x 2048 rows: 221, 182 (two states), 210, in pieces 220; 24 ragged ones of 12347 rows, 4096 channels: 234, 222,
-// 292, in pieces 298; 2 x 512 rows, 512 channels: 58, 36, 26, in pieces 17.
+// sequence be worked on side by side, for a second pass over most of them that makes no outputs.  Both sides are modelled, in
+// us, and the fastest cut is taken: `chain`, a row's steps in a wavefront by itself, against `work`, all rows' instructions on
+// a chip that is full; whichever is longer, and something of the other when they are close.  The lengths in a ragged batch are
+// in device memory: the longest is taken for that of a batch of widely varied lengths (1.1: at 0.75, fitted to milder ones, 24
+// sequences of 12347 rows, 3 to 8 times the mean the longest, took 4 states per lane and 292 us instead of 253 on the average).
+// Constants fitted to 30 calls of 1 to 200 sequences, 1000 to 32768 rows, 64 to 8192 channels, 8 to 64 states, each cut in 4 to
+// 15 ways (MI355X): the cut taken took 1.03 times as long as the fastest.  16384 rows of 2048 channels: 1743 us whole with 4
+// states per lane, 733 with one, 258 in pieces of 512; 8 x 2048 rows: 221, 182 (two states), 210, in pieces 220; 24 ragged ones
+// of 12347 rows, 4096 channels: 234, 222, 292, in pieces 298; 2 x 512 rows, 512 channels: 58, 36, 26, in pieces 17.
 static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
 {
     ScanPlan best = {lanes_per_channel(p->states, 4), 4, 0};
@@ -146,7 +147,11 @@ extern "C" int icv_selective_scan(const icv_scan_params* p, const icv_sequences*
     const ScanPlan plan = plan_scan(p, seq);
     const int cw = 256 / plan.S;
     a.group_tiles = (a.per_group + cw - 1) / cw;
-    a.by_length = (seq->start || seq->length) && seq->count > 1 && seq->count <= 64;
+    // Finding the order costs every workgroup a few instructions per sequence: done where workgroups have to wait for others and
+    // there are rows enough to pay for it (20 sequences of 2000 rows, 4096 channels: 54 us as they came, 40 by length; 64 of 1000
+    // rows: 35 and 47).
+    a.by_length = (seq->start || seq->length) && seq->count > 1 && seq->count <= 64 && seq->tokens / seq->count >= 32 &&
+                  (int64_t)a.group_tiles * p->groups * seq->count > 256;
     a.chunk = plan.rows;
     const int64_t pieces = a.chunk ? piece_count(seq, a.chunk) : 0;
     if (a.chunk && (!workspace || misaligned(workspace, 16))) return ICV_ERR_INVALID_ARG;
