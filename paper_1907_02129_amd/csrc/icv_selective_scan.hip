@@ -28,13 +28,14 @@ static bool hook_fits(int hook, int states)
 // Fewer states per lane shorten the steps that follow one another, for some more instructions in all; pieces let the rows of a
 // sequence be worked on side by side, for a second pass over most of them that makes no outputs.  Both sides are modelled, in
 // us, and the fastest cut is taken: `chain`, a row's steps in a wavefront by itself, against `work`, all rows' instructions on
-// a chip that is full; whichever is longer, and something of the other when they are close.  The lengths in a ragged batch are
-// in device memory: the longest is taken for that of a batch of widely varied lengths (1.1: at 0.75, fitted to milder ones, 24
-// sequences of 12347 rows, 3 to 8 times the mean the longest, took 4 states per lane and 292 us instead of 253 on the average).
-// Constants fitted to 30 calls of 1 to 200 sequences, 1000 to 32768 rows, 64 to 8192 channels, 8 to 64 states, each cut in 4 to
-// 15 ways (MI355X): the cut taken took 1.03 times as long as the fastest.  16384 rows of 2048 channels: 1743 us whole with 4
-// states per lane, 733 with one, 258 in pieces of 512; 8 x 2048 rows: 221, 182 (two states), 210, in pieces 220; 24 ragged ones
-// of 12347 rows, 4096 channels: 234, 222, 292, in pieces 298; 2 x 512 rows, 512 channels: 58, 36, 26, in pieces 17.
+// a chip that is full; whichever is longer, and something of the other when they are close.  A tile's inputs are staged whole,
+// so that sequences shorter than one pay for all of it. The lengths in a ragged batch are in device memory: they are taken for
+// widely varied ones, whose longest has 1 + 1.2 log(count) times the mean (at 0.75, fitted to milder ones, 24 sequences of
+// 12347 rows, 3 to 8 times the mean the longest, took 4 states per lane and 292 us instead of 253 on the average). Constants
+// fitted to 100 calls of 1 to 256 sequences, 30 to 32768 rows, 64 to 8192 channels, 8 to 64 states, each cut in 1 to 15 ways
+// (MI355X): the cut taken took 1.015 times as long as the fastest. 16384 rows of 2048 channels: 1743 us whole with 4 states per
+// lane, 733 with one, 258 in pieces of 512; 8 x 2048 rows: 221, 182 (two states), 210, in pieces 220; 24 ragged ones of 12347
+// rows, 4096 channels: 234, 222, 292, in pieces 298; 2 x 512 rows, 512 channels: 58, 36, 26, in pieces 17.
 static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
 {
     ScanPlan best = {lanes_per_channel(p->states, 4), 4, 0};
@@ -46,27 +47,28 @@ static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
     const int32_t per_group = p->channels / p->groups;
     const bool equal = seq->count == 1 || (!seq->start && !seq->length);
     const double tokens = seq->tokens, mean = tokens / seq->count;
-    const double longest = equal ? mean : fmin(tokens, mean * (1 + 1.1 * log((double)seq->count)));
+    const double longest = equal ? mean : fmin(tokens, mean * (1 + 1.2 * log((double)seq->count)));
     double least = 1e30;
     for (int NS = 4; NS >= 1; NS /= 2) {
         if (NS < 4 && (p->states <= 4 || p->states > 16 * NS)) continue;
         const int S = lanes_per_channel(p->states, NS), cw = 256 / S, tt = 8 * S < 64 ? 8 * S : 64;
         const bool odd = p->states != S * NS || per_group % 2 != 0;
         const double channels = (double)p->groups * ((per_group + cw - 1) / cw) * cw;
-        const double work = tokens * channels * (1.55 + 0.178 * S * NS + 0.104 * S) * 1e-6 * (odd ? 1.3 : 1.0);
-        const double chain = (0.022 + 0.0146 * NS + 0.0745 / S) * (odd ? 1.4 : 1.0);
+        const double staged = seq->count * (equal ? ceil(mean / tt) * tt : tt / (1 - exp(-tt / mean)));       // rows of whole tiles
+        const double work = channels * (1.92 * staged + tokens * (0.171 * S * NS + 0.106 * S)) * 1e-6 * (odd ? 1.3 : 1.0);
+        const double chain = (0.0209 + 0.0134 * NS + 0.0454 / S) * (odd ? 1.4 : 1.0);
         const auto both = [](double a, double b) {
             const double more = fmax(a, b), less = fmin(a, b);
             return more + 0.25 * less * (less / more) * (less / more);
         };
         for (int32_t rows = 0; rows <= 1024; rows = rows ? 2 * rows : 128) {
             if (rows >= (equal ? mean : tokens)) break;
-            double us = 6.6 + both(longest * chain, work);
+            double us = 5.1 + both(longest * chain, work);
             if (rows) {
                 const int32_t r = (rows + tt - 1) / tt * tt;
                 const double whole = seq->count / (tokens / r + 0.5 * seq->count);      // pieces that end a sequence: no first pass
                 const double steps = fmin(longest, r) * chain;
-                us = 8.4 + both(0.7 * steps, 0.3 * work * fmax(0.0, 1 - whole)) + 1.23 * both(steps, work) + longest / r / 8;
+                us = 11 + both(0.7 * steps, 0.2 * work * fmax(0.0, 1 - whole)) + 1.2 * both(steps, work) + longest / r / 8;
             }
             if (us < least) {
                 least = us;
