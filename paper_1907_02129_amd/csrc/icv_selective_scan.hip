@@ -19,10 +19,13 @@ static bool is_step(const icv_sequences* seq) { return !seq->start && seq->token
 // cut on calls small enough for a reference): bits 8-9 1: four states per lane, 2: two, 3: one; bits 10-15 rows per piece in 64s
 // (0: whole sequences).
 static int hook_states_per_lane(int hook) { return 8 >> (hook & 3); }
-static bool hook_fits(int hook, int states)
+// Fewer than four states per lane: where all have enough, and a group has two channels (a thread stages them in pairs).
+static bool fewer_fit(int NS, int states, int per_group) { return states > 4 && states <= 16 * NS && per_group > 1; }
+
+static bool hook_fits(int hook, int states, int per_group)
 {
     const int NS = hook_states_per_lane(hook);
-    return (hook & 3) != 0 && hook < 256 && (NS == 4 || (states > 4 && states <= 16 * NS));
+    return (hook & 3) != 0 && hook < 256 && (NS == 4 || fewer_fit(NS, states, per_group));
 }
 
 // Fewer states per lane shorten the steps that follow one another, for some more instructions in all; pieces let the rows of a
@@ -50,13 +53,13 @@ static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
     const double longest = equal ? mean : fmin(tokens, mean * (1 + 1.2 * log((double)seq->count)));
     double least = 1e30;
     for (int NS = 4; NS >= 1; NS /= 2) {
-        if (NS < 4 && (p->states <= 4 || p->states > 16 * NS)) continue;
+        if (NS < 4 && !fewer_fit(NS, p->states, per_group)) continue;
         const int S = lanes_per_channel(p->states, NS), cw = 256 / S, tt = 8 * S < 64 ? 8 * S : 64;
         const bool odd = p->states != S * NS || per_group % 2 != 0;
         const double channels = (double)p->groups * ((per_group + cw - 1) / cw) * cw;
         const double staged = seq->count * (equal ? ceil(mean / tt) * tt : tt / (1 - exp(-tt / mean)));       // rows of whole tiles
-        const double work = channels * (1.92 * staged + tokens * (0.171 * S * NS + 0.106 * S)) * 1e-6 * (odd ? 1.3 : 1.0);
-        const double chain = (0.0209 + 0.0134 * NS + 0.0454 / S) * (odd ? 1.4 : 1.0);
+        const double work = channels * (1.92 * staged + tokens * (0.171 * S * NS + 0.106 * S)) * 1e-6 * (odd ? 1.15 : 1.0);
+        const double chain = (0.0209 + 0.0134 * NS + 0.0454 / S) * (odd ? 1.15 : 1.0);
         const auto both = [](double a, double b) {
             const double more = fmax(a, b), less = fmin(a, b);
             return more + 0.25 * less * (less / more) * (less / more);
@@ -89,7 +92,7 @@ static int check_scan(const icv_scan_params* p, const icv_sequences* seq, SeqArg
     if (!p || p->channels < 1 || p->states < 1 || p->groups < 1 || p->channels % p->groups != 0) return ICV_ERR_INVALID_ARG;
     if (p->states > 64) return ICV_ERR_UNSUPPORTED;
     if (p->softplus < 0 || (p->softplus & 255) > 1) return ICV_ERR_INVALID_ARG;
-    if (p->softplus >> 8 && !hook_fits(p->softplus >> 8, p->states)) return ICV_ERR_UNSUPPORTED;
+    if (p->softplus >> 8 && !hook_fits(p->softplus >> 8, p->states, p->channels / p->groups)) return ICV_ERR_UNSUPPORTED;
     if (p->dtype == ICV_U8I8) return ICV_ERR_UNSUPPORTED;
     if (p->dtype != ICV_F32 && p->dtype != ICV_BF16) return ICV_ERR_INVALID_ARG;
     for (int32_t r : {p->x_row_stride, p->dt_row_stride, p->z_row_stride, p->out_row_stride})

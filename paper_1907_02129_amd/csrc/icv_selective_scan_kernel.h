@@ -96,10 +96,17 @@ struct Rows {
     float b[R][NS], c[R][NS];
 };
 
-template <typename T, int S, int NS, bool ODD, int MODE>
+// How a row's ends are read. FULL: a lane's states and a thread's pair of channels are all there. PART: where some are not, as
+// many elements from further left in the row, shifted into place when they are staged (24 sequences of 12000 rows, bfloat16,
+// 4095 channels: 282 us; with 4096 246, element by element 339; 15 of 968 rows, 4800 channels, 42 states: 96, element by
+// element 121). ONE_BY_ONE: rows too short to have them (under 4 states, one channel a group).
+enum { FULL = 0, PART = 1, ONE_BY_ONE = 2 };
+
+template <typename T, int S, int NS, int ENDS, int MODE>
 __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
 {
     constexpr int CW = 256 / S, TT = 8 * S < 64 ? 8 * S : 64, PAIRS = CW / 2, RPT = TT * PAIRS / 256, ROWS = TT / RPT;
+    constexpr bool ODD = ENDS != FULL, ONE = ENDS == ONE_BY_ONE;
     constexpr int NP = S * NS, VS = NP / 4;        // states with those that are not there, in vectors of 4
     constexpr int BCV = (TT * VS + 255) / 256;     // vectors of B (and C) a thread stages
     __shared__ __align__(16) float2 dtx[TT][CW];    // delta and delta * x; the row's output takes delta's place
@@ -209,34 +216,37 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
     // row a third of all vector instructions were address arithmetic.
     constexpr uint32_t SZ = sizeof(T);
     const uint32_t vc = c0 + (vn ? vch : 0);
-    const uint32_t xo = (vrow * (uint32_t)a.xs + vc) * SZ, dto = (vrow * (uint32_t)a.dts + vc) * SZ, zo = (vrow * (uint32_t)a.zs + vc) * SZ,
+    const int vshift = ENDS == PART ? 2 - vn : 0;      // 2: a pair of the group's first channels, not used
+    const uint32_t vl = vshift == 2 ? group * a.per_group : vc - vshift;       // channel loaded from
+    const uint32_t xo = (vrow * (uint32_t)a.xs + vl) * SZ, dto = (vrow * (uint32_t)a.dts + vl) * SZ, zo = (vrow * (uint32_t)a.zs + vl) * SZ,
                    oo = vrow * (uint32_t)a.os + vc;
     const auto row_of = [](const void* p, int64_t row, int64_t stride) { return (const uint8_t*)p + row * stride * SZ; };      // scalar
     // Rows past the end repeat the last one (and are made to change nothing when they are staged): loads without branches
     constexpr int BCT = TT * VS < 256 ? TT * VS : 256;              // threads with B and C of their own; the others repeat them
     const int bct = tid % BCT, n4 = 4 * (bct % VS), bcrow = bct / VS;
     const int bcn = a.states - n4 < 0 ? 0 : (a.states - n4 < 4 ? a.states - n4 : 4);
-    const uint32_t bc0 = (uint32_t)group * a.states + (bcn ? n4 : 0);
-    Raw<T, 2, ODD> nx[RPT], nd[RPT], nz[RPT];
-    Raw<T, 4, ODD> nB[BCV], nC[BCV];
+    const int bcshift = ENDS == PART && bcn ? 4 - bcn : 0;
+    const uint32_t bc0 = (uint32_t)group * a.states + (bcn ? n4 - bcshift : 0);
+    Raw<T, 2, ONE> nx[RPT], nd[RPT], nz[RPT];
+    Raw<T, 4, ONE> nB[BCV], nC[BCV];
     auto fetch_tile = [&](int32_t r, auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
         const int32_t most = row1 - 1 - r;
-        const auto pairs = [&](Raw<T, 2, ODD> (&q)[RPT], const void* p, int64_t stride, uint32_t at) {
+        const auto pairs = [&](Raw<T, 2, ONE> (&q)[RPT], const void* p, int64_t stride, uint32_t at) {
 #pragma unroll
             for (int k = 0; k < RPT; k++) {
                 if constexpr (WHOLE) {
                     q[k].load(row_of(p, r + k * ROWS, stride), at, vn);
                 } else {
                     const int32_t row = vrow + k * ROWS;
-                    q[k].load(row_of(p, r, stride), ((uint32_t)(row < most ? row : most) * (uint32_t)stride + vc) * SZ, vn);
+                    q[k].load(row_of(p, r, stride), ((uint32_t)(row < most ? row : most) * (uint32_t)stride + vl) * SZ, vn);
                 }
             }
         };
         pairs(nx, a.x, a.xs, xo);
         pairs(nd, a.dt, a.dts, dto);
         if (MODE != SCAN_PIECE_STATE && a.z) pairs(nz, a.z, a.zs, zo);
-        const auto fours = [&](Raw<T, 4, ODD> (&q)[BCV], const void* p, int64_t stride) {
+        const auto fours = [&](Raw<T, 4, ONE> (&q)[BCV], const void* p, int64_t stride) {
             const uint8_t* base = row_of(p, r, stride);
 #pragma unroll
             for (int k = 0; k < BCV; k++) {
@@ -258,12 +268,17 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
     float total = 0.0f;                       // sum of delta over the piece
     fetch(row0);
     for (int32_t r = row0; r < row1; r += TT) {
-        Raw<T, 2, ODD> cx[RPT], cz[RPT];
+        Raw<T, 2, ONE> cx[RPT], cz[RPT];
         const bool tail = r + TT > row1;
 #pragma unroll
         for (int k = 0; k < RPT; k++) {
             cx[k] = nx[k];
             cz[k] = nz[k];
+            if constexpr (ENDS == PART) {
+                cx[k].align(vshift & 1);
+                cz[k].align(vshift & 1);
+                nd[k].align(vshift & 1);
+            }
             float v[2] = {nd[k].get(0) + dtb[0], nd[k].get(1) + dtb[1]};
             if (a.softplus) { v[0] = softplus(v[0]); v[1] = softplus(v[1]); }
             float4 q = make_float4(v[0], v[0] * cx[k].get(0), v[1], v[1] * cx[k].get(1));
@@ -274,7 +289,8 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
         for (int k = 0; k < BCV; k++) {
             const int row = bcrow + k * (256 / VS);
             const bool out = tail && r + row >= row1;
-            const auto values = [&](const Raw<T, 4, ODD>& q) {
+            const auto values = [&](Raw<T, 4, ONE> q) {
+                if constexpr (ENDS == PART) q.align(bcshift);
                 float4 v = make_float4(q.get(0), q.get(1), q.get(2), q.get(3));
                 if (ODD) v = make_float4(bcn > 0 ? v.x : 0.0f, bcn > 1 ? v.y : 0.0f, bcn > 2 ? v.z : 0.0f, bcn > 3 ? v.w : 0.0f);
                 return out ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : v;
@@ -472,23 +488,27 @@ int launch_step(const ScanArgs& a, hipStream_t s)
     return ICV_OK;
 }
 
+template <typename T, int S, int NS, int ENDS>
+void launch_modes(const ScanArgs& a, uint32_t n, hipStream_t s)
+{
+    if (!a.chunk) {
+        k_scan<T, S, NS, ENDS, SCAN_WHOLE><<<n, 256, 0, s>>>(a);
+        return;
+    }
+    k_scan<T, S, NS, ENDS, SCAN_PIECE_STATE><<<n, 256, 0, s>>>(a);
+    k_scan<T, S, NS, ENDS, SCAN_PIECE_OUT><<<n, 256, 0, s>>>(a);
+}
+
 template <typename T, int S, int NS>
 int launch(const ScanArgs& a, hipStream_t s)
 {
-    const bool odd = a.states != NS * S || a.per_group % 2 != 0;
+    const bool full = a.states == NS * S && a.per_group % 2 == 0;
     const int64_t n = (int64_t)a.group_tiles * (a.channels / a.per_group) * (a.chunk ? a.units : a.seq.count);
     if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-    if (!a.chunk) {
-        if (odd) k_scan<T, S, NS, true, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
-        else k_scan<T, S, NS, false, SCAN_WHOLE><<<(uint32_t)n, 256, 0, s>>>(a);
-        ICV_HIP_CHECK(hipGetLastError());
-        return ICV_OK;
-    }
-    if (odd) k_scan<T, S, NS, true, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
-    else k_scan<T, S, NS, false, SCAN_PIECE_STATE><<<(uint32_t)n, 256, 0, s>>>(a);
-    ICV_HIP_CHECK(hipGetLastError());
-    if (odd) k_scan<T, S, NS, true, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
-    else k_scan<T, S, NS, false, SCAN_PIECE_OUT><<<(uint32_t)n, 256, 0, s>>>(a);
+    const bool one = a.states < 4 || a.per_group == 1;
+    if (full) launch_modes<T, S, NS, FULL>(a, (uint32_t)n, s);
+    else if (NS == 4 && one) launch_modes<T, S, 4, ONE_BY_ONE>(a, (uint32_t)n, s);       // and never with fewer states per lane
+    else launch_modes<T, S, NS, PART>(a, (uint32_t)n, s);
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;
 }

@@ -111,6 +111,25 @@ struct Raw {
             }
         }
     }
+    // Loaded whole from `shift` elements before: the first N - shift are put in their places.
+    __device__ void align(int shift)
+    {
+        static_assert(!ODD && (N == 2 || N == 4), "");
+        if constexpr (sizeof(T) == 4) {
+            if (shift & 1)
+#pragma unroll
+                for (int j = 0; j + 1 < N; j++) w[j] = w[j + 1];
+            if (N > 2 && shift & 2)
+#pragma unroll
+                for (int j = 0; j + 2 < N; j++) w[j] = w[j + 2];
+        } else if constexpr (N == 2) {
+            w[0] >>= 16 * shift;
+        } else {
+            const uint64_t v = (w[0] | (uint64_t)w[1] << 32) >> (16 * shift);
+            w[0] = (uint32_t)v;
+            w[1] = (uint32_t)(v >> 32);
+        }
+    }
 };
 
 // v / (1 + exp(-v)).  exp(-v) overflows to infinity below -88, which gives -0, the limit; the reciprocal is the

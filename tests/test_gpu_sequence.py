@@ -167,6 +167,15 @@ def test_selective_scan_state_sizes(states, dtype):
         scan_case(BATCHES[name], 21, states, 3, dtype, True, True, True, 1, states)
 
 
+@pytest.mark.parametrize("channels,groups", [(1, 1), (2, 1), (5, 5), (10, 5), (65, 1), (129, 1), (33, 11)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_selective_scan_narrow_groups(channels, groups, dtype):
+    """Rows whose ends are read from further left or one by one: groups of one to three channels, one channel past a tile."""
+    for states in (1, 3, 4, 7, 16):
+        scan_case(BATCHES["packed"], channels, states, groups, dtype, True, True, True, 0, states)
+        scan_case(BATCHES["one_long"], channels, states, groups, dtype, True, False, False, 1, states, scale=0.1, hook=1 | 1 << 2)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("per_lane,states", [(4, 4), (4, 3), (4, 8), (4, 6), (4, 16), (4, 12), (4, 32), (4, 29), (4, 64), (4, 47),
                                              (2, 8), (2, 5), (2, 16), (2, 13), (2, 32), (2, 20), (1, 8), (1, 7), (1, 16), (1, 10)])
