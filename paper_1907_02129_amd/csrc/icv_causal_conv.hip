@@ -67,10 +67,17 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
     // the last sequence that begins at or before the run's first row, else the first one
     int32_t i = 0;
     if (a.seq.start) {
-        int32_t lo = 0, hi = a.seq.count;              // begin(lo) <= r0 < begin(hi), if any begins there
+        // begin(lo) <= r0 < begin(hi), if any begins there; seven places at a time, since each round waits for memory once
+        int32_t lo = 0, hi = a.seq.count;
         while (hi - lo > 1) {
-            const int32_t mid = (lo + hi) >> 1;
-            if (seq_begin(a.seq, mid) <= r0) lo = mid; else hi = mid;
+            const int32_t step = (hi - lo + 7) >> 3;
+            int32_t at[7], n = 0;
+#pragma unroll
+            for (int k = 0; k < 7; k++) at[k] = a.seq.start[lo + (k + 1) * step < hi ? lo + (k + 1) * step : lo];
+#pragma unroll
+            for (int k = 0; k < 7; k++) n += lo + (k + 1) * step < hi && clamp_row(at[k], a.seq.tokens) <= r0;
+            lo += n * step;
+            hi = lo + step < hi ? lo + step : hi;
         }
         i = lo;
     } else {
@@ -88,26 +95,36 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
         if (owner && hi < own_end) hi = own_end;
         if (lo >= hi) continue;
 
+        // everything that is read first is on its way together: the rows before the first one, AHEAD rows, the rows of the new state
         float win[W > 1 ? W - 1 : 1][VEC];
-        int32_t from = -1;
-        Row q[AHEAD > W - 1 ? AHEAD : W - 1];
-        if (owner) {
-            from = a.state ? seq_slot(a.seq, a.seq.from, i) : -1;
-            if (from >= 0)
+        Row before[W > 1 ? W - 1 : 1], q[AHEAD], last[W > 1 ? W - 1 : 1];
+        const int32_t from = owner && a.state ? seq_slot(a.seq, a.seq.from, i) : -1, slot = owner && a.state ? seq_slot(a.seq, a.seq.to, i) : -1;
+        const auto fetch = [&](int32_t t0) {            // past the end the last one again
 #pragma unroll
-                for (int k = 0; k < W - 1; k++) take(q[k], state + from * a.slot_stride + (int64_t)k * a.channels, nv);
-        } else {
+            for (int u = 0; u < AHEAD; u++) take(q[u], in + (int64_t)(t0 + u < hi ? t0 + u : hi - 1) * a.in_stride, nv);
+        };
+        fetch(lo);
+        if (from >= 0) {
 #pragma unroll
-            for (int k = 0; k < W - 1; k++) take(q[k], in + (int64_t)(lo - (W - 1) + k) * a.in_stride, nv);
+            for (int k = 0; k < W - 1; k++) take(before[k], state + from * a.slot_stride + (int64_t)k * a.channels, nv);
+        } else if (!owner) {
+#pragma unroll
+            for (int k = 0; k < W - 1; k++) take(before[k], in + (int64_t)(lo - (W - 1) + k) * a.in_stride, nv);
+        }
+        if (slot >= 0) {
+#pragma unroll
+            for (int k = 0; k < W - 1; k++) {
+                const int32_t at = e - b - (W - 1) + k;  // the sequence's row that becomes state row k; below 0 an old one
+                take(last[k], at < 0 && from >= 0 ? state + from * a.slot_stride + (int64_t)(W - 1 + at) * a.channels
+                                                  : in + (int64_t)(b + (at > 0 ? at : 0)) * a.in_stride, nv);
+            }
         }
 #pragma unroll
         for (int k = 0; k < W - 1; k++)
 #pragma unroll
-            for (int j = 0; j < VEC; j++) win[k][j] = owner && from < 0 ? 0.0f : q[k].get(j);
-        // AHEAD rows on their way at once; past the end the last one again
+            for (int j = 0; j < VEC; j++) win[k][j] = owner && from < 0 ? 0.0f : before[k].get(j);
         for (int32_t t0 = lo; t0 < hi; t0 += AHEAD) {
-#pragma unroll
-            for (int u = 0; u < AHEAD; u++) take(q[u], in + (int64_t)(t0 + u < hi ? t0 + u : hi - 1) * a.in_stride, nv);
+            if (t0 > lo) fetch(t0);
 #pragma unroll
             for (int u = 0; u < AHEAD; u++) {
                 if (t0 + u >= hi) break;
@@ -135,22 +152,12 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
                 }
             }
         }
-        const int32_t slot = owner && a.state ? seq_slot(a.seq, a.seq.to, i) : -1;
-        if (W > 1 && slot >= 0) {
+        if (slot >= 0) {
 #pragma unroll
             for (int k = 0; k < W - 1; k++) {
-                const int32_t at = e - b - (W - 1) + k;  // the sequence's row that becomes state row k; below 0 an old one
                 float v[VEC];
 #pragma unroll
-                for (int j = 0; j < VEC; j++) v[j] = 0.0f;
-                // an old row moves down, and none is overwritten before it has
-                const T* p = at >= 0 ? in + (int64_t)(b + at) * a.in_stride
-                                     : (from >= 0 ? state + from * a.slot_stride + (int64_t)(W - 1 + at) * a.channels : nullptr);
-                if (p) {
-                    take(q[0], p, nv);
-#pragma unroll
-                    for (int j = 0; j < VEC; j++) v[j] = q[0].get(j);
-                }
+                for (int j = 0; j < VEC; j++) v[j] = e - b - (W - 1) + k < 0 && from < 0 ? 0.0f : last[k].get(j);
                 store_row<VEC>(state + slot * a.slot_stride + (int64_t)k * a.channels, ODD ? nv : VEC, v);
             }
         }
