@@ -165,17 +165,20 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
 }
 
 // Rows per run: 32, and fewer until there are 2048 wavefronts (two for every SIMD): a run reads taps - 1 rows more
-// than it computes (12347 rows, 4096 channels: 50.4 us with 32, 52.5 with 16; 32 alone would leave 64 rows of 2048 channels to 16 wavefronts).
+// than it computes (12347 rows, 4096 channels: 50.4 us with 32, 52.5 with 16; 32 alone would leave 64 rows of 2048 channels to 16
+// wavefronts).  Under 4 where sequences are short, since a thread goes through its run's one after another (156 of 341 rows, 72
+// channels: 10.6 us with 4, 7.9 with 2, 5.0 with 1), not where they are long (33 of 2707 rows, 768 channels: 6.7 with 4, 7.8 with 2).
 template <typename T, int W>
 static int launch(ConvArgs a, hipStream_t s)
 {
     constexpr int VEC = 8 / sizeof(T);
     a.vecs = (a.channels + VEC - 1) / VEC;
     const bool single = !a.seq.start && a.seq.each == 1;
+    const int32_t least = a.seq.tokens / a.seq.count >= 16 ? 4 : 1;
     int64_t threads = 0;
     for (a.run = single ? 1 : 32;; a.run /= 2) {
         threads = (int64_t)a.vecs * (((int64_t)a.seq.tokens + a.run - 1) / a.run);
-        if (a.run <= 4 || threads >= 2048 * 64) break;
+        if (a.run <= least || threads >= 2048 * 64) break;
     }
     const int64_t blocks = (threads + 255) / 256;
     if (blocks > INT32_MAX - 8) return ICV_ERR_INVALID_ARG;
