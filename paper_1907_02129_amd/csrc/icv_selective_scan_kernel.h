@@ -410,10 +410,11 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
 // sequences: a wavefront alone waits for the slot number, then for the state, then ends; with Q states on their way together
 // the compute units' wavefronts cover that: 128 sequences, 4096 channels, 16 states, bfloat16 15.8 us, 4.5 TB/s, with two; 16.8 with
 // one, 16.1 with four.  Loads have no branches around them (a sequence that continues no slot reads slot 0 and
-// drops it; 18.5 us with branches).
-template <typename T, int S, bool ODD, int Q>
+// drops it; 18.5 us with branches).  89 sequences, 2560 channels, 40 states: 21 us; element by element 40.
+template <typename T, int S, int ENDS, int Q>
 __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
 {
+    constexpr bool ODD = ENDS != FULL, ONE = ENDS == ONE_BY_ONE;
     constexpr int CW = 256 / S;
     const int tid = threadIdx.x, lane = tid & 63;
     const int32_t tiles = (a.channels + CW - 1) / CW;
@@ -423,8 +424,9 @@ __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
     const int32_t d = tile * CW + (tid >> 6) * (64 / S) + wch;
     if (d >= a.channels) return;                      // whole channels, so whole exchange partners
     const int nv = a.states - 4 * s < 0 ? 0 : (a.states - 4 * s < 4 ? a.states - 4 * s : 4);
+    const int shift = ENDS == PART && nv ? 4 - nv : 0;
     const uint32_t n4 = nv ? 4 * s : 0;
-    const int64_t state_at = (int64_t)d * a.states + n4, bc = (int64_t)(d / a.per_group) * a.states + n4;
+    const int64_t state_at = (int64_t)d * a.states + n4, first_at = state_at - shift, bc = (int64_t)(d / a.per_group) * a.states + n4 - shift;
     const bool slots = a.state && a.seq.slots > 0;
 
     int32_t seq[Q], src[Q], dst[Q];
@@ -436,14 +438,14 @@ __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
         src[q] = slots ? seq_slot(a.seq, a.seq.from, seq[q]) : -1;
         dst[q] = slots && on[q] ? seq_slot(a.seq, a.seq.to, seq[q]) : -1;
     }
-    Raw<float, 4, ODD> hr[Q], Ar;
-    Raw<T, 4, ODD> br[Q], cr[Q];
+    Raw<float, 4, ONE> hr[Q], Ar;
+    Raw<T, 4, ONE> br[Q], cr[Q];
     Raw<T, 1, false> xr[Q], dr[Q], zr[Q];
     const auto at = [](const void* p, int64_t element, size_t size) { return (const uint8_t*)p + element * (int64_t)size; };
-    Ar.load(at(a.A, state_at, 4), 0, nv);
+    Ar.load(at(a.A, first_at, 4), 0, nv);
 #pragma unroll
     for (int q = 0; q < Q; q++) {
-        if (slots) hr[q].load(at(a.state, (src[q] >= 0 ? src[q] : 0) * a.slot_stride + state_at, 4), 0, nv);
+        if (slots) hr[q].load(at(a.state, (src[q] >= 0 ? src[q] : 0) * a.slot_stride + first_at, 4), 0, nv);
         br[q].load(at(a.B, seq[q] * a.bs + bc, sizeof(T)), 0, nv);
         cr[q].load(at(a.C, seq[q] * a.cs + bc, sizeof(T)), 0, nv);
         xr[q].load(at(a.x, seq[q] * a.xs + d, sizeof(T)), 0, 1);
@@ -451,8 +453,14 @@ __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
         if (a.z) zr[q].load(at(a.z, seq[q] * a.zs + d, sizeof(T)), 0, 1);
     }
     const float dtb = a.dtb ? a.dtb[d] : 0.0f, D = a.D ? a.D[d] : 0.0f;
+    if constexpr (ENDS == PART) Ar.align(shift);
 #pragma unroll
     for (int q = 0; q < Q; q++) {
+        if constexpr (ENDS == PART) {
+            hr[q].align(shift);
+            br[q].align(shift);
+            cr[q].align(shift);
+        }
         float dt = dr[q].get(0) + dtb, y = 0.0f, h[4];
         const float x = xr[q].get(0);
         if (a.softplus) dt = softplus(dt);
@@ -478,12 +486,15 @@ int launch_step(const ScanArgs& a, hipStream_t s)
 {
     constexpr int CW = 256 / S;
     const int64_t tiles = (a.channels + CW - 1) / CW, wgs = tiles * a.seq.count;
-    const bool two = wgs >= 2048 && a.states == 4 * S;      // more than the chip holds at once
+    const bool two = wgs >= 2048 && a.states >= 4;      // more than the chip holds at once
     const int64_t n = two ? tiles * (((int64_t)a.seq.count + 1) / 2) : wgs;
     if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-    if (a.states != 4 * S) k_scan_step<T, S, true, 1><<<(uint32_t)n, 256, 0, s>>>(a);
-    else if (two) k_scan_step<T, S, false, 2><<<(uint32_t)n, 256, 0, s>>>(a);
-    else k_scan_step<T, S, false, 1><<<(uint32_t)n, 256, 0, s>>>(a);
+    if (a.states != 4 * S) {
+        if constexpr (S == 1) k_scan_step<T, S, ONE_BY_ONE, 1><<<(uint32_t)n, 256, 0, s>>>(a);
+        else if (two) k_scan_step<T, S, PART, 2><<<(uint32_t)n, 256, 0, s>>>(a);
+        else k_scan_step<T, S, PART, 1><<<(uint32_t)n, 256, 0, s>>>(a);
+    } else if (two) k_scan_step<T, S, FULL, 2><<<(uint32_t)n, 256, 0, s>>>(a);
+    else k_scan_step<T, S, FULL, 1><<<(uint32_t)n, 256, 0, s>>>(a);
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;
 }

@@ -189,11 +189,11 @@ def test_selective_scan_every_cut(per_lane, states, dtype):
     scan_case(BATCHES["one_long"], 21, states, 3, dtype, False, False, False, 0, states, scale=0.1, hook=code | 2 << 2)
 
 
-@pytest.mark.parametrize("states", [4, 8, 16, 32, 64])
+@pytest.mark.parametrize("states", [4, 8, 16, 32, 64, 2, 5, 15, 26, 61])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_single_tokens_of_more_sequences_than_the_chip_holds(states, dtype):
     """Two sequences to a workgroup, an odd number of them, some without rows, some without a slot."""
-    count, channels = 259, 8 * 64 if states == 16 else {4: 2048, 8: 1024, 32: 256, 64: 128}[states]
+    count, channels = 259, {4: 2048, 8: 1024, 16: 512, 32: 256, 64: 128, 2: 2048, 5: 1022, 15: 510, 26: 254, 61: 126}[states]
     g = gen(states)
     lengths = (torch.rand(count, generator=g) < 0.9).int().tolist()
     batch = Batch(lengths, "step", source=[i if i % 5 else -1 for i in range(count)], target=[count + i if i % 7 else 10 ** 6 for i in range(count)],
