@@ -28,11 +28,11 @@ struct ConvArgs {
     SeqArgs seq;
 };
 
-template <typename T, int W, int VEC, int AHEAD, bool ODD>
+template <typename T, int W, int VEC, int AHEAD, int ENDS>
 __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
 {
-    using Row = Raw<T, VEC, ODD>;
-    const auto take = [](Row& q, const T* p, int n) { q.load((const uint8_t*)p, 0, n); };
+    constexpr bool ODD = ENDS != FULL;
+    using Row = Raw<T, VEC, ENDS == ONE_BY_ONE>;
     // workgroups go to the 8 XCDs in turn: each gets neighbouring runs, so that the rows in front of a run are in its L2
     const int64_t id = ((int64_t)(blockIdx.x & 7) * a.per_xcd + (blockIdx.x >> 3)) * 256 + threadIdx.x;
     const int32_t runs = (a.seq.tokens - 1) / a.run + 1;
@@ -40,6 +40,12 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
     if (r >= runs) return;
     const int32_t c0 = (int32_t)(id - r * a.vecs) * VEC;
     const int32_t nv = a.channels - c0 < VEC ? a.channels - c0 : VEC;
+    const int shift = ENDS == PART ? VEC - nv : 0;
+    const auto take = [&](Row& q, const T* p, int n) { q.load((const uint8_t*)(p - shift), 0, n); };
+    const auto align = [&](auto& rows) {
+        if constexpr (ENDS == PART)
+            for (auto& q : rows) q.align(shift);
+    };
     const T* in = (const T*)a.in + c0;
     T* out = (T*)a.out + c0;
     T* state = (T*)a.state + c0;
@@ -119,12 +125,14 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
                                                   : in + (int64_t)(b + (at > 0 ? at : 0)) * a.in_stride, nv);
             }
         }
+        align(before);
 #pragma unroll
         for (int k = 0; k < W - 1; k++)
 #pragma unroll
             for (int j = 0; j < VEC; j++) win[k][j] = owner && from < 0 ? 0.0f : before[k].get(j);
         for (int32_t t0 = lo; t0 < hi; t0 += AHEAD) {
             if (t0 > lo) fetch(t0);
+            align(q);
 #pragma unroll
             for (int u = 0; u < AHEAD; u++) {
                 if (t0 + u >= hi) break;
@@ -153,6 +161,7 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
             }
         }
         if (slot >= 0) {
+            align(last);
 #pragma unroll
             for (int k = 0; k < W - 1; k++) {
                 float v[VEC];
@@ -164,30 +173,36 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
     }
 }
 
+template <typename T, int W, int VEC, int ENDS>
+static void launch_ahead(const ConvArgs& a, bool single, hipStream_t s)
+{
+    if (single) k_causal_conv<T, W, VEC, 1, ENDS><<<8 * a.per_xcd, 256, 0, s>>>(a);
+    else k_causal_conv<T, W, VEC, 4, ENDS><<<8 * a.per_xcd, 256, 0, s>>>(a);
+}
+
 // Rows per run: 32, and fewer until there are 2048 wavefronts (two for every SIMD): a run reads taps - 1 rows more
 // than it computes (12347 rows, 4096 channels: 50.4 us with 32, 52.5 with 16; 32 alone would leave 64 rows of 2048 channels to 16
-// wavefronts).  Under 4 where sequences are short, since a thread goes through its run's one after another (156 of 341 rows, 72
-// channels: 10.6 us with 4, 7.9 with 2, 5.0 with 1), not where they are long (33 of 2707 rows, 768 channels: 6.7 with 4, 7.8 with 2).
+// wavefronts).  Under 4 that costs more than half as much again and 1024 wavefronts are enough (33 sequences of 2707 rows, 768 channels: 6.7
+// us with 4, 7.8 with 2; 20 of 3000 rows, 3 channels: 8.9 with 4, 6.0 with 1), except where sequences are short, which a thread goes
+// through one after another (214 of 299 rows, 2048 channels: 9.6 with 4, 7.8 with 2, 6.1 with 1).
 template <typename T, int W>
 static int launch(ConvArgs a, hipStream_t s)
 {
     constexpr int VEC = 8 / sizeof(T);
     a.vecs = (a.channels + VEC - 1) / VEC;
     const bool single = !a.seq.start && a.seq.each == 1;
-    const int32_t least = a.seq.tokens / a.seq.count >= 16 ? 4 : 1;
+    const bool short_ones = a.seq.tokens / a.seq.count < 16;
     int64_t threads = 0;
     for (a.run = single ? 1 : 32;; a.run /= 2) {
         threads = (int64_t)a.vecs * (((int64_t)a.seq.tokens + a.run - 1) / a.run);
-        if (a.run <= least || threads >= 2048 * 64) break;
+        if (a.run == 1 || threads >= (a.run > 4 || short_ones ? 2048 : 1024) * 64) break;
     }
     const int64_t blocks = (threads + 255) / 256;
     if (blocks > INT32_MAX - 8) return ICV_ERR_INVALID_ARG;
     a.per_xcd = (int32_t)((blocks + 7) / 8);
-    const bool odd = a.channels % VEC != 0;
-    if (single && odd) k_causal_conv<T, W, VEC, 1, true><<<8 * a.per_xcd, 256, 0, s>>>(a);
-    else if (single) k_causal_conv<T, W, VEC, 1, false><<<8 * a.per_xcd, 256, 0, s>>>(a);
-    else if (odd) k_causal_conv<T, W, VEC, 4, true><<<8 * a.per_xcd, 256, 0, s>>>(a);
-    else k_causal_conv<T, W, VEC, 4, false><<<8 * a.per_xcd, 256, 0, s>>>(a);
+    if (a.channels % VEC == 0) launch_ahead<T, W, VEC, FULL>(a, single, s);
+    else if (a.channels >= VEC) launch_ahead<T, W, VEC, PART>(a, single, s);
+    else launch_ahead<T, W, VEC, ONE_BY_ONE>(a, single, s);
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;
 }

@@ -96,12 +96,6 @@ struct Rows {
     float b[R][NS], c[R][NS];
 };
 
-// How a row's ends are read. FULL: a lane's states and a thread's pair of channels are all there. PART: where some are not, as
-// many elements from further left in the row, shifted into place when they are staged (24 sequences of 12000 rows, bfloat16,
-// 4095 channels: 282 us; with 4096 246, element by element 339; 15 of 968 rows, 4800 channels, 42 states: 96, element by
-// element 121). ONE_BY_ONE: rows too short to have them (under 4 states, one channel a group).
-enum { FULL = 0, PART = 1, ONE_BY_ONE = 2 };
-
 template <typename T, int S, int NS, int ENDS, int MODE>
 __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
 {
