@@ -275,7 +275,9 @@ ICV_API int icv_conv2d_nhwc_im2col_static(const icv_conv_params* p, const void* 
  * undefined.  A slot may be continued by several sequences; a slot that a sequence writes must not be read or written
  * by another one of the same call (reading and writing the same slot by one sequence is the usual case).
  * One new token per sequence is tokens == count without `start`.
- * count = 0 or tokens = 0: nothing to do, ICV_OK.  tokens > 2^31 - 2^16: ICV_ERR_UNSUPPORTED.
+ * count = 0 or tokens = 0: nothing to do, ICV_OK.  tokens > 2^31 - 2^16: ICV_ERR_UNSUPPORTED; so is, here and in the
+ * 8-bit operators, a call that would take 2^32 threads (a scan takes up to 16 a channel and sequence, at least 256 a
+ * group and sequence, and so many for each piece; the others come to it with more than 100 GB of rows).
  */
 typedef struct icv_sequences {
     int32_t count;

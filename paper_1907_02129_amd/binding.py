@@ -323,7 +323,10 @@ def _load_native():
 
 def _call(name, first, stream, *args):
     """The operator on the first tensor's device: on the given stream, which must be that device's, or its current one."""
-    device = first.get_device()
+    try:
+        device = first.get_device()
+    except AttributeError:
+        raise TypeError(f"icv_{name}: a tensor expected, got {type(first)}") from None
     if device < 0:
         raise ValueError("icv takes device tensors")
     if stream is None:

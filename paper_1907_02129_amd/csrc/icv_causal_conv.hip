@@ -76,7 +76,7 @@ __global__ __launch_bounds__(256) void k_causal_conv(ConvArgs a)
         // begin(lo) <= r0 < begin(hi), if any begins there; seven places at a time, since each round waits for memory once
         int32_t lo = 0, hi = a.seq.count;
         while (hi - lo > 1) {
-            const int32_t step = (hi - lo + 7) >> 3;
+            const int32_t step = ((hi - lo - 1) >> 3) + 1;
             int32_t at[7], n = 0;
 #pragma unroll
             for (int k = 0; k < 7; k++) at[k] = a.seq.start[lo + (k + 1) * step < hi ? lo + (k + 1) * step : lo];
@@ -198,7 +198,7 @@ static int launch(ConvArgs a, hipStream_t s)
         if (a.run == 1 || threads >= (a.run > 4 || short_ones ? 2048 : 1024) * 64) break;
     }
     const int64_t blocks = (threads + 255) / 256;
-    if (blocks > INT32_MAX - 8) return ICV_ERR_INVALID_ARG;
+    if (too_many(blocks + 7, 256)) return ICV_ERR_UNSUPPORTED;
     a.per_xcd = (int32_t)((blocks + 7) / 8);
     if (a.channels % VEC == 0) launch_ahead<T, W, VEC, FULL>(a, single, s);
     else if (a.channels >= VEC) launch_ahead<T, W, VEC, PART>(a, single, s);

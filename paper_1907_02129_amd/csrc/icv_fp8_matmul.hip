@@ -9,6 +9,7 @@
 // the difference being power); to float 890.  8 x 4096, 2048 deep: 4.8 us, a launch; 8 x 4096, 8192 deep 10.6, 3.2 TB/s of filter;
 // 64 x 8192, 4096 deep 11.5; 1024 x 4096, 4096 deep 26, 1.3 PFLOP/s.
 #include "icv_mfma_common.h"
+#include "icv_sequence.h"
 #include <cmath>
 
 namespace icv {
@@ -384,7 +385,7 @@ static int launch_tile(MatmulArgs g, hipStream_t s)
     g.col_tiles = (uint32_t)((g.cols + (int64_t)BN - 1) / BN);
     g.row_tiles = (uint32_t)((g.rows + (int64_t)BM - 1) / BM);
     const int64_t n = (int64_t)g.col_tiles * g.row_tiles;
-    if (n > INT32_MAX / 2) return ICV_ERR_INVALID_ARG;
+    if (too_many(n + 7, 64 * WN * WM * KG)) return ICV_ERR_UNSUPPORTED;
     g.tiles = (uint32_t)n;
     g.per_xcd = (uint32_t)((n + 7) / 8);
     const auto kernel = k_matmul_tile<OUT, BN, BM, WN, WM, KG, AHEAD>;
@@ -398,7 +399,7 @@ template <typename OUT, int WAVES>
 static int launch_split(const MatmulArgs& g, hipStream_t s)
 {
     const int64_t n = ((g.cols + (int64_t)15) / 16) * ((g.rows + (int64_t)15) / 16);
-    if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
+    if (too_many(n, 64 * WAVES)) return ICV_ERR_UNSUPPORTED;
     k_matmul_split<OUT, WAVES><<<(uint32_t)n, 64 * WAVES, 0, s>>>(g);
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;
@@ -474,8 +475,8 @@ extern "C" int icv_matmul_fp8(const icv_matmul_params* p, const void* a, const f
     if (p->out_row_stride && p->out_row_stride < p->cols) return ICV_ERR_INVALID_ARG;
     if (p->rows == 0) return ICV_OK;
     if (!a || !a_scales || !b || !b_scales || !out) return ICV_ERR_INVALID_ARG;
-    const auto off = [](const void* q, uintptr_t bytes) { return ((uintptr_t)q & (bytes - 1)) != 0; };
-    if (off(a, 16) || off(b, 16) || off(a_scales, 4) || off(b_scales, 4) || off(bias, 4) || off(out, out_type == ICV_OUT_ACC ? 4 : 2))
+    if (misaligned(a, 16) || misaligned(b, 16) || misaligned(a_scales, 4) || misaligned(b_scales, 4) || misaligned(bias, 4) ||
+        misaligned(out, out_type == ICV_OUT_ACC ? 4 : 2))
         return ICV_ERR_INVALID_ARG;
     if (out == a || out == b) return ICV_ERR_INVALID_ARG;
     MatmulArgs g = {(const uint8_t*)a, (const uint8_t*)b, a_scales, b_scales, bias, out, p->rows, p->cols, blocks, (p->cols + 127) / 128,

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
 #pragma unroll
     for (int j = 0; j < NS; j++) {
         A[j] *= kLog2e;
-        A[j] = A[j] < -3.0e38f ? -3.0e38f : A[j];     // rows past the end step by 0 * A, which has to be 0
+        A[j] = A[j] < -3.0e38f ? -3.0e38f : (A[j] > 3.0e38f ? 3.0e38f : A[j]);     // rows past the end step by 0 * A, which has to be 0
     }
 
     const int64_t state_at = (int64_t)d * a.states + NS * s;
@@ -482,7 +482,7 @@ int launch_step(const ScanArgs& a, hipStream_t s)
     const int64_t tiles = (a.channels + CW - 1) / CW, wgs = tiles * a.seq.count;
     const bool two = wgs >= 2048 && a.states >= 4;      // more than the chip holds at once
     const int64_t n = two ? tiles * (((int64_t)a.seq.count + 1) / 2) : wgs;
-    if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
+    if (too_many(n, 256)) return ICV_ERR_UNSUPPORTED;
     if (a.states != 4 * S) {
         if constexpr (S == 1) k_scan_step<T, S, ONE_BY_ONE, 1><<<(uint32_t)n, 256, 0, s>>>(a);
         else if (two) k_scan_step<T, S, PART, 2><<<(uint32_t)n, 256, 0, s>>>(a);
@@ -509,7 +509,7 @@ int launch(const ScanArgs& a, hipStream_t s)
 {
     const bool full = a.states == NS * S && a.per_group % 2 == 0;
     const int64_t n = (int64_t)a.group_tiles * (a.channels / a.per_group) * (a.chunk ? a.units : a.seq.count);
-    if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
+    if (too_many(n, 256)) return ICV_ERR_UNSUPPORTED;
     const bool one = a.states < 4 || a.per_group == 1;
     if (full) launch_modes<T, S, NS, FULL>(a, (uint32_t)n, s);
     else if (NS == 4 && one) launch_modes<T, S, 4, ONE_BY_ONE>(a, (uint32_t)n, s);       // and never with fewer states per lane

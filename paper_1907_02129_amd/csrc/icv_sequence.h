@@ -26,6 +26,9 @@ inline int make_seq_args(const icv_sequences* s, int32_t slots, SeqArgs* a)
     return ICV_OK;
 }
 
+// A launch's threads are counted in 32 bits.
+inline bool too_many(int64_t workgroups, int threads) { return workgroups > (int64_t)UINT32_MAX / threads; }
+
 inline bool misaligned(const void* p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1)) != 0; }
 
 __device__ inline int32_t clamp_row(int32_t v, int32_t tokens) { return v < 0 ? 0 : (v > tokens ? tokens : v); }
@@ -120,21 +123,22 @@ struct Raw {
     // Loaded whole from `shift` elements before: the first N - shift are put in their places.
     __device__ void align(int shift)
     {
-        static_assert(!ODD && (N == 2 || N == 4), "");
-        if constexpr (sizeof(T) == 4) {
-            if (shift & 1)
-#pragma unroll
-                for (int j = 0; j + 1 < N; j++) w[j] = w[j + 1];
-            if (N > 2 && shift & 2)
-#pragma unroll
-                for (int j = 0; j + 2 < N; j++) w[j] = w[j + 2];
-        } else if constexpr (N == 2) {
-            w[0] >>= 16 * shift;
-        } else {
+        static_assert(WORDS, "");
+        constexpr int WN = sizeof(w) / 4, PER = 4 / sizeof(T);
+        if constexpr (PER == 2 && N == 4) {
             const uint64_t v = (w[0] | (uint64_t)w[1] << 32) >> (16 * shift);
             w[0] = (uint32_t)v;
             w[1] = (uint32_t)(v >> 32);
+            return;
         }
+        if (PER == 2 && shift & 1)
+#pragma unroll
+            for (int j = 0; j < WN; j++) w[j] = w[j] >> 16 | (j + 1 < WN ? w[j + 1] << 16 : 0);
+#pragma unroll
+        for (int by = 1; by < WN; by *= 2)
+            if (shift & by * PER)
+#pragma unroll
+                for (int j = 0; j + by < WN; j++) w[j] = w[j + by];
     }
 };
 

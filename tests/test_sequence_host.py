@@ -183,10 +183,24 @@ def test_pointers_of_the_8_bit_operators_are_checked(lib):
     assert lib.icv_matmul_fp8(None, ADDRESS, ADDRESS, ADDRESS, ADDRESS, None, ADDRESS, None) == BAD
 
 
+def test_calls_of_too_many_threads_are_refused(lib):
+    many = 1 << 30
+    assert conv(lib, seq(many, many), channels=1 << 20) == UNSUPPORTED
+    assert conv(lib, seq(1, many), channels=1 << 24, dtype=icv.ICV_F32) == UNSUPPORTED
+    assert scan(lib, seq(many, many), channels=4096) == UNSUPPORTED                        # single tokens
+    assert scan(lib, seq(many // 2, many), channels=4096) == UNSUPPORTED
+    assert quantize(lib, rows=2 ** 31 - 1, depth=1 << 20) == UNSUPPORTED
+    assert quantize(lib, rows=2 ** 31 - 1, depth=1 << 24, block_rows=128) == UNSUPPORTED
+    for out in (icv.ICV_OUT_ACC, icv.ICV_OUT_BF16):
+        assert matmul(lib, rows=2 ** 31 - 1, cols=1 << 30, out_type=out) == UNSUPPORTED
+
+
 def test_the_binding_refuses_host_tensors():
     x = torch.zeros(4, 16, dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         icv.causal_conv1d(icv.make_causal_conv_params(16, 4), seq(1, 4), x, x, None, None, x)
+    with pytest.raises(TypeError, match="a tensor expected"):
+        icv.causal_conv1d(icv.make_causal_conv_params(16, 4), seq(1, 4), [1.0], x, None, None, x)
     with pytest.raises(ValueError):
         icv.make_sequences(1, 4, start=torch.zeros(2, dtype=torch.int32))
     with pytest.raises(ValueError):
