@@ -1,8 +1,9 @@
 // Quantisation into e4m3 with a scale per block of 128 columns and 1 or 128 rows (icv_quantize_fp8).
 //
-// Memory bound: every element is read once and leaves as one byte.  Sixteen lanes take a row's block of 128, 8 elements
-// each, so the maximum of a row's block is four exchanges within a row of 16 lanes, and a wavefront covers four
-// neighbouring blocks of a row.  12288 x 4096 from bfloat16: 31.7 us, 4.8 TB/s (a copy: 5.2).
+// Memory bound: every element is read once and leaves as one byte. Sixteen lanes take a row's block of 128, 8 elements each, so
+// the maximum of a row's block is four exchanges within a row of 16 lanes, and a wavefront covers four neighbouring blocks of a
+// row. 12288 x 4096 with a scale a row from bfloat16 27 us, 5.6 TB/s, from float 37, 6.8 TB/s, both partly from cache (with
+// other data in between 31 and 4.8 TB/s; a copy: 5.2 TB/s); 4100 deep, where rows begin anywhere, 30 and 40.
 #include "icv_sequence.h"
 
 namespace icv {
@@ -73,7 +74,7 @@ __device__ inline uint2 encode8(const float (&v)[8], const Divider& by)
 }
 
 // A wavefront takes R rows of four neighbouring blocks of columns.
-template <typename T, int R, bool ODD>
+template <typename T, int R, int ENDS>
 __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a)
 {
     const int lane = threadIdx.x & 63;
@@ -84,17 +85,19 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a)
     if (strip * R >= a.rows || block >= a.blocks) return;        // whole rows of 16 lanes
     const int32_t r0 = (int32_t)(strip * R), c = block * 128 + (lane & 15) * 8;
     const int n = a.depth - c < 0 ? 0 : (a.depth - c < 8 ? a.depth - c : 8);
+    const int shift = ENDS == PART && n ? 8 - n : 0;
     float scale[R];
-    Raw<T, 8, ODD> raw[R];
+    Raw<T, 8, ENDS == ONE_BY_ONE> raw[R];
 #pragma unroll
     for (int r = 0; r < R; r++)
-        raw[r].load((const uint8_t*)((const T*)a.in + (int64_t)(r0 + r < a.rows ? r0 + r : r0) * a.in_stride + (n ? c : 0)), 0, n);
+        raw[r].load((const uint8_t*)((const T*)a.in + (int64_t)(r0 + r < a.rows ? r0 + r : r0) * a.in_stride + (n ? c - shift : 0)), 0, n);
 #pragma unroll
     for (int r = 0; r < R; r++) {
         float v[8], m = 0.0f;
+        if constexpr (ENDS == PART) raw[r].align(shift);
 #pragma unroll
         for (int j = 0; j < 8; j++) {
-            v[j] = (ODD ? j < n : n > 0) ? raw[r].get(j) : 0.0f;
+            v[j] = (ENDS != FULL ? j < n : n > 0) ? raw[r].get(j) : 0.0f;
             m = fmaxf(m, fabsf(v[j]));
         }
         scale[r] = scale_of(row16_max(m));
@@ -107,7 +110,7 @@ __global__ __launch_bounds__(256) void k_quantize_rows(QuantArgs a)
 }
 
 // A workgroup takes a block of 128 x 128: 16 rows at a time, 8 elements a lane, all held until the maximum is known.
-template <typename T, bool ODD>
+template <typename T, int ENDS>
 __global__ __launch_bounds__(256) void k_quantize_blocks(QuantArgs a)
 {
     __shared__ float part[4];
@@ -115,14 +118,18 @@ __global__ __launch_bounds__(256) void k_quantize_blocks(QuantArgs a)
     const int32_t block = (int32_t)(blockIdx.x % a.blocks), strip = (int32_t)(blockIdx.x / a.blocks);
     const int32_t c = block * 128 + (tid & 15) * 8, row_blocks = (a.rows - 1) / 128 + 1;
     const int n = a.depth - c < 0 ? 0 : (a.depth - c < 8 ? a.depth - c : 8);
-    Raw<T, 8, ODD> raw[8];
+    const int shift = ENDS == PART && n ? 8 - n : 0;
+    Raw<T, 8, ENDS == ONE_BY_ONE> raw[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) {
         const int64_t r = (int64_t)strip * 128 + i * 16 + (tid >> 4);
-        raw[i].load((const uint8_t*)((const T*)a.in + (r < a.rows ? r : a.rows - 1) * a.in_stride + (n ? c : 0)), 0, n);
+        raw[i].load((const uint8_t*)((const T*)a.in + (r < a.rows ? r : a.rows - 1) * a.in_stride + (n ? c - shift : 0)), 0, n);
     }
     float m = 0.0f;
-    const auto value = [&](int i, int j) { return (ODD ? j < n : n > 0) ? raw[i].get(j) : 0.0f; };      // rows past the end: the last again
+    const auto value = [&](int i, int j) { return (ENDS != FULL ? j < n : n > 0) ? raw[i].get(j) : 0.0f; };      // rows past the end: the last again
+    if constexpr (ENDS == PART)
+#pragma unroll
+        for (int i = 0; i < 8; i++) raw[i].align(shift);
 #pragma unroll
     for (int i = 0; i < 8; i++)
 #pragma unroll
@@ -151,14 +158,16 @@ static int launch(const QuantArgs& a, int block_rows, hipStream_t s)
     if (block_rows == 1) {
         constexpr int R = 2;       // 12288 x 4096 bfloat16: 31.7 us; 33.6 with one row, 31.4 with four, which leaves short batches fewer wavefronts
         const int64_t waves = (int64_t)((a.blocks + 3) / 4) * ((a.rows - 1) / R + 1), n = (waves + 3) / 4;
-        if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-        if (a.depth % 8) k_quantize_rows<T, R, true><<<(uint32_t)n, 256, 0, s>>>(a);
-        else k_quantize_rows<T, R, false><<<(uint32_t)n, 256, 0, s>>>(a);
+        if (too_many(n, 256)) return ICV_ERR_UNSUPPORTED;
+        if (a.depth % 8 == 0) k_quantize_rows<T, R, FULL><<<(uint32_t)n, 256, 0, s>>>(a);
+        else if (a.depth >= 8) k_quantize_rows<T, R, PART><<<(uint32_t)n, 256, 0, s>>>(a);
+        else k_quantize_rows<T, R, ONE_BY_ONE><<<(uint32_t)n, 256, 0, s>>>(a);
     } else {
         const int64_t n = (int64_t)a.blocks * ((a.rows - 1) / 128 + 1);
-        if (n > INT32_MAX) return ICV_ERR_INVALID_ARG;
-        if (a.depth % 8) k_quantize_blocks<T, true><<<(uint32_t)n, 256, 0, s>>>(a);
-        else k_quantize_blocks<T, false><<<(uint32_t)n, 256, 0, s>>>(a);
+        if (too_many(n, 256)) return ICV_ERR_UNSUPPORTED;
+        if (a.depth % 8 == 0) k_quantize_blocks<T, FULL><<<(uint32_t)n, 256, 0, s>>>(a);
+        else if (a.depth >= 8) k_quantize_blocks<T, PART><<<(uint32_t)n, 256, 0, s>>>(a);
+        else k_quantize_blocks<T, ONE_BY_ONE><<<(uint32_t)n, 256, 0, s>>>(a);
     }
     ICV_HIP_CHECK(hipGetLastError());
     return ICV_OK;

@@ -36,7 +36,7 @@ def quantized(x, block_rows, dtype, pad=0, code_pad=0):
 
 
 @pytest.mark.parametrize("rows", [1, 2, 5, 127, 128, 129, 300])
-@pytest.mark.parametrize("depth", [1, 7, 8, 128, 129, 515, 1024])
+@pytest.mark.parametrize("depth", [1, 7, 8, 9, 12, 13, 14, 15, 128, 129, 250, 515, 1024])
 @pytest.mark.parametrize("block_rows", [1, 128])
 def test_quantize_sizes(rows, depth, block_rows):
     for dtype in ("bf16", "f32"):
