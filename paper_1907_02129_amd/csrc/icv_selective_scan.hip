@@ -29,16 +29,17 @@ static bool hook_fits(int hook, int states, int per_group)
 }
 
 // Fewer states per lane shorten the steps that follow one another, for some more instructions in all; pieces let the rows of a
-// sequence be worked on side by side, for a second pass over most of them that makes no outputs.  Both sides are modelled, in
+// sequence be worked on side by side, for a second pass over most of them that makes no outputs. Both sides are modelled, in
 // us, and the fastest cut is taken: `chain`, a row's steps in a wavefront by itself, against `work`, all rows' instructions on
-// a chip that is full; whichever is longer, and something of the other when they are close.  A tile's inputs are staged whole,
+// a chip that is full; whichever is longer, and something of the other when they are close. A tile's inputs are staged whole,
 // so that sequences shorter than one pay for all of it. The lengths in a ragged batch are in device memory: they are taken for
 // widely varied ones, whose longest has 1 + 1.2 log(count) times the mean (at 0.75, fitted to milder ones, 24 sequences of
 // 12347 rows, 3 to 8 times the mean the longest, took 4 states per lane and 292 us instead of 253 on the average). Constants
 // fitted to 100 calls of 1 to 256 sequences, 30 to 32768 rows, 64 to 8192 channels, 8 to 64 states, each cut in 1 to 15 ways
 // (MI355X): the cut taken took 1.015 times as long as the fastest. 16384 rows of 2048 channels: 1743 us whole with 4 states per
 // lane, 733 with one, 258 in pieces of 512; 8 x 2048 rows: 221, 182 (two states), 210, in pieces 220; 24 ragged ones of 12347
-// rows, 4096 channels: 234, 222, 292, in pieces 298; 2 x 512 rows, 512 channels: 58, 36, 26, in pieces 17.
+// rows, 4096 channels: 234, 222, 292, in pieces 298; 2 x 512 rows, 512 channels: 58, 36, 26, in pieces 17; one of 1065 rows,
+// 1048 channels: 127, 76, 54, in pieces of 128 27, of 64 23.
 static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
 {
     ScanPlan best = {lanes_per_channel(p->states, 4), 4, 0};
@@ -64,7 +65,7 @@ static ScanPlan plan_scan(const icv_scan_params* p, const icv_sequences* seq)
             const double more = fmax(a, b), less = fmin(a, b);
             return more + 0.25 * less * (less / more) * (less / more);
         };
-        for (int32_t rows = 0; rows <= 1024; rows = rows ? 2 * rows : 128) {
+        for (int32_t rows = 0; rows <= 1024; rows = rows ? 2 * rows : 64) {
             if (rows >= (equal ? mean : tokens)) break;
             double us = 5.1 + both(longest * chain, work);
             if (rows) {
