@@ -6,8 +6,8 @@
 // the 4 outputs that a lane holds, which are neighbouring columns of one row).
 //
 // 12288 x 8192, 4096 deep to bfloat16: 390 us, 2.1 PFLOP/s (the vendor's product without block scales: 346; with operands of zeros 351,
-// the difference being power); to float 890.  8 x 4096, 2048 deep: 4.8 us, a launch; 8 x 4096, 8192 deep 10.6, 3.2 TB/s of filter;
-// 64 x 8192, 4096 deep 11.5; 1024 x 4096, 4096 deep 26, 1.3 PFLOP/s.
+// the difference being power); to float 735.  8 x 4096, 2048 deep: 4.8 us, a launch; 8 x 4096, 8192 deep 10.6, 3.2 TB/s of filter;
+// 64 x 8192, 4096 deep 11.5; 2048 x 4096, 4096 deep 41, 1.7 PFLOP/s.
 #include "icv_mfma_common.h"
 #include "icv_sequence.h"
 #include <cmath>
@@ -405,24 +405,36 @@ static int launch_split(const MatmulArgs& g, hipStream_t s)
     return ICV_OK;
 }
 
-// The kernels a product can run on, and what each takes, in us, fitted to 60 products of 1 to 16384 rows, 64 to 16384
-// columns and depth (MI355X, operands not in L2): `alone` for a step (a block of the reduction of every group) where a
-// compute unit has no more than one workgroup, `busy` for each step of each workgroup where it has more, `out` for a tile's
-// outputs.  The fastest by this model took 1.04 times as long as the fastest measured; leaving the 128 x 64 tile out
-// 1.05, the tiles of 32 x 64 whose 4 groups share the reduction 1.12 (64 rows, 8192 columns, 4096 deep: 11.5 us, 15.5 with 64 x 64).
-// Float outputs have no 256 x 256 tile: widened operands leave no room in the registers (5284 x 6015, 256 deep: 49.6 us, 38.3 with
-// 128 x 64).
+// The kernels a product can run on, and what each takes, in us, fitted to 114 products of 1 to 20000 rows, 64 to 16384 columns
+// and depth (MI355X, operands not in L2): `step` for a step (a block of the reduction of every group) where a compute unit has
+// one workgroup, `more` on top for each further one beside it, up to `resident`, `rest` for a workgroup's beginning and
+// outputs. The busiest compute unit has ceil(tiles / 256) workgroups, `resident` at a time; the mean counts for a part
+// (`kBusiest`), since the lighter ones leave it power and bandwidth. The fastest by this model took 1.006 times as long as the
+// fastest measured. With as much for each further workgroup as for the first that was 1.04: 498 rows, 12734 columns, 4096 deep,
+// 400 tiles of 128 x 128, two to most compute units, 37 us, 47 with the 128 x 64 taken then; 2048 x 4096, 4096 deep 40 and 51.
+// Leaving the tiles of 32 x 64 out, whose 4 groups share the reduction: 64 rows, 8192 columns, 4096 deep 11.5 us, 15.5 with 64
+// x 64. Float outputs have no 256 x 256 tile: widened operands leave no room in the registers (5284 x 6015, 256 deep: 49.6 us,
+// 38.3 with 128 x 64).
 constexpr int64_t kMostTileStride = 1 << 23;       // the tile kernels keep a tile's offsets in 32 bits
+constexpr double kBusiest[2] = {0.75, 0.86};       // by output, bfloat16 and float
 struct MatmulKernel {
-    int32_t cols, rows, groups;
-    double alone, busy, out;
+    int32_t cols, rows, groups, resident;
+    double step, more, rest;
 };
 enum { TILE_256 = 0, TILE_128, TILE_128_64, TILE_64, TILE_32_64, SPLIT, KERNELS };
 static const MatmulKernel kKernels[2][KERNELS] = {
-    {{256, 256, 1, 2.5, 2.5, 2.0}, {128, 128, 1, 0.78, 1.05, 0.71}, {128, 64, 1, 0.51, 0.50, 0.42}, {64, 64, 1, 0.35, 0.27, 0.26},
-     {32, 64, 4, 0.64, 1.36, 0.25}, {16, 16, 8, 0.65, 0.61, 0.0}},
-    {{256, 256, 1, 1e9, 1e9, 0.0}, {128, 128, 1, 1.14, 1.80, 1.03}, {128, 64, 1, 0.72, 0.85, 0.54}, {64, 64, 1, 0.48, 0.52, 0.22},
-     {32, 64, 4, 0.93, 1.83, 0.11}, {16, 16, 8, 0.62, 0.67, 0.0}}};
+    {{256, 256, 1, 1, 2.30, 0.0, 2.68}, {128, 128, 1, 2, 0.807, 0.481, 1.07}, {128, 64, 1, 3, 0.513, 0.301, 0.672},
+     {64, 64, 1, 4, 0.325, 0.182, 0.548}, {32, 64, 4, 1, 0.717, 0.0, 0.481}, {16, 16, 8, 4, 0.743, 0.873, 0.0}},
+    {{256, 256, 1, 1, 1e9, 0.0, 0.0}, {128, 128, 1, 2, 1.06, 1.14, 2.03}, {128, 64, 1, 3, 0.790, 0.552, 0.870},
+     {64, 64, 1, 4, 0.429, 0.337, 0.502}, {32, 64, 4, 1, 1.14, 0.0, 0.222}, {16, 16, 8, 4, 0.674, 0.627, 0.0}}};
+
+// What a compute unit takes for n workgroups, a part of one counting as that.
+static double compute_unit_us(const MatmulKernel& m, double steps, double n)
+{
+    const double rounds = floor(n / m.resident), left = n - rounds * m.resident;
+    return rounds * (steps * (m.step + (m.resident - 1) * m.more) + m.rest) +
+           fmin(left, 1.0) * (steps * (m.step + fmax(left - 1.0, 0.0) * m.more) + m.rest);
+}
 
 // `hook`: a test hook, bits 8-11 of icv_matmul_params::out_type (icv.h says they must be 0; the library's own tests set them to run
 // every kernel on products small enough for a reference): 1 + the kernel.
@@ -436,8 +448,8 @@ static int choose_kernel(const MatmulArgs& g, bool exact, int hook)
         const MatmulKernel& m = kKernels[exact][k];
         const double tiles = (double)((g.cols + (int64_t)m.cols - 1) / m.cols) * (double)((g.rows + (int64_t)m.rows - 1) / m.rows);
         const double steps = (double)((g.blocks + m.groups - 1) / m.groups);
-        const double turns = k == TILE_256 ? ceil(tiles / 256) : tiles / 256;      // one workgroup per compute unit, or several
-        const double us = fmax(steps * m.alone, turns * steps * m.busy) + fmax(turns, 1.0) * m.out;
+        const double mean = fmax(tiles / 256, 1.0);
+        const double us = kBusiest[exact] * compute_unit_us(m, steps, ceil(mean)) + (1 - kBusiest[exact]) * compute_unit_us(m, steps, mean);
         if (us < least) { least = us; best = k; }
     }
     return best;
