@@ -3,7 +3,7 @@
 // Per row, channel and state: one exponential (the decay), two products and two multiply-adds.  Vector-ALU bound: 24 issue
 // cycles for 64 of them (8 for the exponential, 4 for each of the others), and about 40 instructions per row and channel around
 // them (softplus, gate, conversions), against 2 to 8 bytes of memory per row and channel.  24 sequences of 12347 rows, 4096
-// channels, 16 states, bfloat16 with gate: 231 us, 1.8 TB/s, about what the instructions alone take; up to 335 where one sequence has a
+// channels, 16 states, bfloat16 with gate: 223 to 265 us, 1.8 TB/s, about what the instructions alone take; 310 where one sequence has a
 // third of the rows, whose steps follow one another (525 us at first: what was in the way were waits for the next tile's loads
 // inside conversions and branches, 64-bit address products, bank conflicts, and the longest sequence).
 //
