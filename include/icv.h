@@ -316,7 +316,8 @@ ICV_API int icv_causal_conv1d(const icv_causal_conv_params* p, const icv_sequenc
  *   delta = dt[t][d] + dt_bias[d], through log(1 + exp(.)) with softplus
  *   h[d][n] = exp(delta * A[d][n]) * h[d][n] + delta * x[t][d] * B[t][g][n]
  *   y[t][d] = sum_n C[t][g][n] * h[d][n] + D[d] * x[t][d],  times z / (1 + exp(-z)) of z[t][d] where z is given
- * All in float (states, decays, sums); y is rounded once, at the store.
+ * All in float (states, decays, sums); y is rounded once, at the store.  Coefficients A past 2.07e38 in size, infinite ones among
+ * them, count as that: a step of delta = 0 keeps the state whatever A, and a delta of 1e-36 or more forgets it at A = -infinity.
  *   x, dt, z, out : [tokens] rows of channels; z may be NULL.  out may be x, dt or z where the row strides agree
  *   B, C          : [tokens] rows of groups * states
  *   A             : [channels][states] float; D, dt_bias: channels floats, or NULL

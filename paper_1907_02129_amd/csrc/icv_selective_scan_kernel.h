@@ -32,6 +32,14 @@ __device__ inline float softplus(float v)
     return fmaxf(v, 0.0f) + fmaf(__builtin_amdgcn_logf(u), kLn2, e - (u - 1.0f));
 }
 
+// A coefficient as a power of two's, kept finite, so that a step of 0 times it is 0: such a step keeps the state, and the
+// rows past a sequence's end step by 0.  NaN stays NaN.
+__device__ inline float decay_rate(float a)
+{
+    a *= kLog2e;
+    return a < -3.0e38f ? -3.0e38f : (a > 3.0e38f ? 3.0e38f : a);
+}
+
 // lane -> its place among the S lanes of a channel, and the channel among the wavefront's.  The four lowest states of a
 // channel sit in one quad; with 8 lanes the second quad is 8 lanes away, with 16 all of a row of 16 is one channel's,
 // so that the sums over quads are rotations within a row.
@@ -164,10 +172,7 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
     float A[NS], h[NS];
     load_row<NS>(a.A + (int64_t)d * a.states + NS * s, nv, A);
 #pragma unroll
-    for (int j = 0; j < NS; j++) {
-        A[j] *= kLog2e;
-        A[j] = A[j] < -3.0e38f ? -3.0e38f : (A[j] > 3.0e38f ? 3.0e38f : A[j]);     // rows past the end step by 0 * A, which has to be 0
-    }
+    for (int j = 0; j < NS; j++) A[j] = decay_rate(A[j]);
 
     const int64_t state_at = (int64_t)d * a.states + NS * s;
     const int64_t plane = (int64_t)a.channels * a.states;
@@ -448,6 +453,9 @@ __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
     }
     const float dtb = a.dtb ? a.dtb[d] : 0.0f, D = a.D ? a.D[d] : 0.0f;
     if constexpr (ENDS == PART) Ar.align(shift);
+    float A[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) A[j] = decay_rate(Ar.get(j));
 #pragma unroll
     for (int q = 0; q < Q; q++) {
         if constexpr (ENDS == PART) {
@@ -461,7 +469,7 @@ __global__ __launch_bounds__(256) void k_scan_step(ScanArgs a)
 #pragma unroll
         for (int j = 0; j < 4; j++) {
             const float old = src[q] >= 0 ? hr[q].get(j) : 0.0f;
-            h[j] = fmaf(__builtin_amdgcn_exp2f(dt * Ar.get(j) * kLog2e), old, dt * x * br[q].get(j));
+            h[j] = fmaf(__builtin_amdgcn_exp2f(dt * A[j]), old, dt * x * br[q].get(j));
             if (!ODD || j < nv) y = fmaf(cr[q].get(j), h[j], y);
         }
         if (dst[q] >= 0) store_row<4>(a.state + dst[q] * a.slot_stride + state_at, nv, h);

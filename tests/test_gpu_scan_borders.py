@@ -1,0 +1,65 @@
+"""The selective scan at the borders of what its coefficients and cuts allow: infinite and growing decays, every mapping of
+workgroups to sequences, against the definition in 64 bits (sequence_reference) or exact whole numbers."""
+import pytest
+import torch
+
+import sequence_reference as ref
+from paper_1907_02129_amd import binding as icv
+
+pytestmark = pytest.mark.gpu
+# icv_scan_params::softplus above its public value: four, two or one states a lane, whole sequences or pieces of 64 rows
+CUTS = {"auto": 0, "four": 1, "two": 2, "one": 3, "four_pieces": 1 | 1 << 2, "two_pieces": 2 | 1 << 2, "one_pieces": 3 | 1 << 2}
+
+
+def ints(v):
+    return None if v is None else torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def scan(x, dt, A, B, C, state, count, start=None, source=None, target=None, softplus=False, hook=0):
+    """One call on dense float tensors: the output, the state slots and the workspace's size."""
+    n, channels = x.shape
+    seq = icv.make_sequences(count, n, ints(start), None, ints(source), ints(target))
+    p = icv.make_scan_params(channels, A.shape[1], "f32", B.shape[1] // A.shape[1], softplus, state_slots=len(state))
+    p.softplus |= hook << 8
+    space = icv.selective_scan_workspace_bytes(p, seq)
+    ws = torch.full((space // 4,), float("nan"), device="cuda") if space else None
+    st, out = state.cuda(), torch.zeros(n, channels, device="cuda")
+    icv.selective_scan(p, seq, x.cuda(), dt.cuda(), A.cuda(), B.cuda(), C.cuda(), None, None, None, st, out, ws)
+    torch.cuda.synchronize()
+    return out.cpu(), st.cpu(), space
+
+
+@pytest.mark.parametrize("cut", [*CUTS, "step"])
+@pytest.mark.parametrize("states", [16, 13])
+@pytest.mark.parametrize("softplus", [False, True])
+def test_infinite_coefficients_keep_the_state_over_steps_of_zero(cut, states, softplus):
+    """A step of 0 keeps the state whatever its coefficient, any other step with a coefficient of -infinity or the lowest
+    value forgets it.  Steps of 0 and 64 (which log(1 + exp(.)) leaves as it is) and small whole numbers make every state and
+    output a whole number below 2^24, so that they have to be met exactly."""
+    g = torch.Generator().manual_seed(states)
+    n, ch = (9, 20) if cut == "step" else (300, 20)
+    count = n if cut == "step" else 2
+    whole = lambda *shape: torch.randint(-3, 4, shape, generator=g).float()  # noqa: E731
+    x, B, C = whole(n, ch), whole(n, states), whole(n, states)
+    delta = 64.0 * (torch.rand(n, ch, generator=g) < 0.2)
+    delta[:, 1] = 0                              # whole pieces of steps of 0
+    delta[60:200, 2] = 0
+    delta[:, ch - 1] = 0
+    dt = torch.where(delta > 0, delta, torch.full((), -200.0)) if softplus else delta
+    A = torch.full((ch, states), -float("inf"))
+    A[::3], A[:, 5] = -torch.finfo(torch.float32).max, -float("inf")
+    A[ch - 1] = float("inf")                     # of steps of 0 alone
+    state = whole(count, ch, states)
+    slots = list(range(count))
+    start = None if cut == "step" else [0, 170, 300]
+    out, st, space = scan(x, dt, A, B, C, state, count, start, slots, slots, softplus, 0 if cut == "step" else CUTS[cut])
+    assert cut == "auto" or (space > 0) == cut.endswith("pieces")
+    want, want_state = torch.zeros(n, ch, dtype=torch.float64), state.double().clone()
+    for i in range(count):
+        for t in range(i, i + 1) if start is None else range(start[i], start[i + 1]):
+            new = (delta[t] * x[t]).double()[:, None] * B[t].double()
+            want_state[i] = torch.where(delta[t][:, None] > 0, new, want_state[i])
+            want[t] = (want_state[i] * C[t].double()).sum(1)
+    assert want.abs().max() < 2 ** 24 and want_state.abs().max() < 2 ** 24
+    assert torch.equal(st.double(), want_state)
+    assert torch.equal(out.double(), want)
