@@ -40,6 +40,16 @@ __device__ inline float decay_rate(float a)
     return a < -3.0e38f ? -3.0e38f : (a > 3.0e38f ? 3.0e38f : a);
 }
 
+// h * 2^(2 e) + w.  Over a piece's rows 2^(2 e) may be past float's range, up or down, though no state ever is: taken as two
+// factors, and never infinite, so that a state of 0 stays 0 (states below 2^-126 may grow too little past 2^254).  What is lost of
+// a NaN in e, w has: its step or its coefficient made all of the piece NaN.  16384 rows of 2048 channels, whose pieces begin with up to
+// 31 of these for every state: 237.6 us, with one factor 234.8.
+__device__ inline float grow(float h, float e, float w)
+{
+    const float f = __builtin_amdgcn_exp2f(__builtin_amdgcn_fmed3f(e, -126.0f, 127.0f));
+    return fmaf(h * f, f, w);
+}
+
 // lane -> its place among the S lanes of a channel, and the channel among the wavefront's.  The four lowest states of a
 // channel sit in one quad; with 8 lanes the second quad is 8 lanes away, with 16 all of a row of 16 is one channel's,
 // so that the sums over quads are rotations within a row.
@@ -197,7 +207,7 @@ __global__ __launch_bounds__(256) void k_scan(ScanArgs a)
             for (int u = 0; u < 8; u++)
                 if (q0 + u < piece)
 #pragma unroll
-                    for (int j = 0; j < NS; j++) h[j] = fmaf(__builtin_amdgcn_exp2f(sum[u] * A[j]), h[j], w[u][j]);
+                    for (int j = 0; j < NS; j++) h[j] = grow(h[j], sum[u] * (0.5f * A[j]), w[u][j]);
         }
     }
 

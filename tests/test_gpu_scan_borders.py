@@ -63,3 +63,30 @@ def test_infinite_coefficients_keep_the_state_over_steps_of_zero(cut, states, so
     assert want.abs().max() < 2 ** 24 and want_state.abs().max() < 2 ** 24
     assert torch.equal(st.double(), want_state)
     assert torch.equal(out.double(), want)
+@pytest.mark.parametrize("cut", [c for c in CUTS if c != "auto"] + ["four_128", "one_128"])
+def test_decays_over_a_piece_past_the_range_of_float(cut):
+    """Growing states (positive coefficients) whose growth over a piece is past 2^128, though no state ever is: states of zeros stay
+    zeros, tiny ones grow to ordinary ones; and states that fall by more than 2^-128 over a piece and grow again."""
+    n, ch, N = 256 + 20, 12, 8
+    g = torch.Generator().manual_seed(3)
+    hook = {"four_128": 1 | 2 << 2, "one_128": 3 | 2 << 2}.get(cut) or CUTS[cut]
+    x, B, C = torch.zeros(n, ch), torch.rand(n, N, generator=g) + 0.5, torch.rand(n, N, generator=g) + 0.5
+    dt, A, state = torch.ones(n, ch), torch.zeros(ch, N), torch.zeros(2, ch, N)
+    # channels 0..3: 2^260 or more over 128 rows, nothing there until the last 20 rows
+    A[:4] = torch.rand(4, N, generator=g) + 1.5
+    x[256:, :4] = torch.randn(20, 4, generator=g)
+    # channels 4..7: from 2^-120 or so by 2^2.1 a row for 90 rows
+    A[4:8] = 1.46
+    state[0, 4:8] = torch.exp2(-120 + torch.rand(4, N, generator=g))
+    dt[90:, 4:8] = 0
+    # channels 8..11: steps of -1 in the first 64 rows, then of +1: down by 2^-130 and up again (no state falls below 2^-126)
+    A[8:] = 1.41
+    dt[:64, 8:], dt[128:, 8:] = -1, 0
+    state[0, 8:] = 2.0 ** 8 * (1 + torch.rand(4, N, generator=g))
+    out, st, space = scan(x, dt, A, B, C, state, 1, [0, n], [0], [1], False, hook)
+    assert (space > 0) == (hook >> 2 > 0)
+    want, bound, st_want, sbound = ref.selective_scan(x, dt, A, B, C, None, None, None, state, [(0, n)], [0], [1], 1, False, torch.zeros(n, ch),
+                                                      torch.float32, n if space else 0)
+    assert want.isfinite().all() and bound.isfinite().all()
+    ref.check("out", out, want, bound)
+    ref.check("state", st, st_want, sbound)
