@@ -185,18 +185,25 @@ static void launch_ahead(const ConvArgs& a, bool single, hipStream_t s)
 // wavefronts).  Under 4 that costs more than half as much again and 1024 wavefronts are enough (33 sequences of 2707 rows, 768 channels: 6.7
 // us with 4, 7.8 with 2; 20 of 3000 rows, 3 channels: 8.9 with 4, 6.0 with 1), except where sequences are short, which a thread goes
 // through one after another (214 of 299 rows, 2048 channels: 9.6 with 4, 7.8 with 2, 6.1 with 1).
+static int32_t rows_per_run(const ConvArgs& a, bool single)
+{
+    const bool short_ones = a.seq.tokens / a.seq.count < 16;
+    for (int32_t run = single ? 1 : 32;; run /= 2) {
+        const int64_t threads = (int64_t)a.vecs * (((int64_t)a.seq.tokens + run - 1) / run);
+        if (run == 1 || threads >= (run > 4 || short_ones ? 2048 : 1024) * 64) return run;
+    }
+}
+
+// a.run on the way in: a test hook, bits 8-13 of icv_causal_conv_params::silu (icv.h says they must be 0; the library's own tests set
+// them to have runs of several rows and sequences in calls small enough for a reference): the rows per run, 0: the rule's.
 template <typename T, int W>
 static int launch(ConvArgs a, hipStream_t s)
 {
     constexpr int VEC = 8 / sizeof(T);
     a.vecs = (a.channels + VEC - 1) / VEC;
     const bool single = !a.seq.start && a.seq.each == 1;
-    const bool short_ones = a.seq.tokens / a.seq.count < 16;
-    int64_t threads = 0;
-    for (a.run = single ? 1 : 32;; a.run /= 2) {
-        threads = (int64_t)a.vecs * (((int64_t)a.seq.tokens + a.run - 1) / a.run);
-        if (a.run == 1 || threads >= (a.run > 4 || short_ones ? 2048 : 1024) * 64) break;
-    }
+    if (!a.run) a.run = rows_per_run(a, single);
+    const int64_t threads = (int64_t)a.vecs * (((int64_t)a.seq.tokens + a.run - 1) / a.run);
     const int64_t blocks = (threads + 255) / 256;
     if (too_many(blocks + 7, 256)) return ICV_ERR_UNSUPPORTED;
     a.per_xcd = (int32_t)((blocks + 7) / 8);
@@ -228,7 +235,8 @@ extern "C" int icv_causal_conv1d(const icv_causal_conv_params* p, const icv_sequ
                                  const void* filter, const float* bias, void* state, void* output, void* stream)
 {
     using namespace icv;
-    if (!p || p->channels < 1 || p->taps < 1 || p->taps > 8 || (p->silu != 0 && p->silu != 1)) return ICV_ERR_INVALID_ARG;
+    if (!p || p->channels < 1 || p->taps < 1 || p->taps > 8 || p->silu < 0 || (p->silu & 255) > 1) return ICV_ERR_INVALID_ARG;
+    if (p->silu >> 8 > 32) return ICV_ERR_UNSUPPORTED;
     if (p->dtype == ICV_U8I8) return ICV_ERR_UNSUPPORTED;
     if (p->dtype != ICV_F32 && p->dtype != ICV_BF16) return ICV_ERR_INVALID_ARG;
     if ((p->in_row_stride && p->in_row_stride < p->channels) || (p->out_row_stride && p->out_row_stride < p->channels))
@@ -245,7 +253,7 @@ extern "C" int icv_causal_conv1d(const icv_causal_conv_params* p, const icv_sequ
         misaligned(bias, 4))
         return ICV_ERR_INVALID_ARG;
     a.in = input; a.filt = filter; a.bias = bias; a.state = state; a.out = output;
-    a.channels = p->channels; a.silu = p->silu;
+    a.channels = p->channels; a.silu = p->silu & 255; a.run = p->silu >> 8;
     a.in_stride = p->in_row_stride ? p->in_row_stride : p->channels;
     a.out_stride = p->out_row_stride ? p->out_row_stride : p->channels;
     a.slot_stride = p->state_slot_stride ? p->state_slot_stride : slot;

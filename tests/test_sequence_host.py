@@ -232,3 +232,9 @@ def test_the_checks_name_what_is_wrong():
     other.device = 1
     with pytest.raises(ValueError, match="one device"):
         native.causal_conv1d(0, 0, p, other, x, x, None, None, x)
+
+
+def test_rows_per_run_that_no_convolution_has(lib):
+    for hook in (33, 64, 1 << 20):                                                      # test hooks
+        assert conv(lib, silu=1 | hook << 8) == UNSUPPORTED
+    assert conv(lib, silu=-1) == BAD and conv(lib, silu=4 << 8 | 2) == BAD
