@@ -1,11 +1,11 @@
 """The operators on sequences on the paths that large batches take, on batches small enough for the reference: convolution runs of
-several rows and sequences, rooms with a start and a length."""
+several rows and sequences, scans of the longest sequences first, pieces of more than 64 sequences, rooms with a start and a length."""
 import pytest
 import torch
 
 import sequence_reference as ref
 from paper_1907_02129_amd import binding as icv
-from test_gpu_sequence import Batch, conv_case, gen
+from test_gpu_sequence import Batch, conv_case, gen, scan_case
 
 pytestmark = pytest.mark.gpu
 
@@ -80,3 +80,43 @@ def test_convolution_of_a_large_ragged_batch(dtype, channels):
     conv_case(Batch(lengths, "packed", tail=37, source=[i if i % 2 else -1 for i in range(24)], target=[24 + i for i in range(24)], slots=48),
               channels, 4, dtype, True, True, True, 0, 3)
     conv_case(rooms(lengths, 9, 4), channels, 3, dtype, False, True, True, 1, 4)
+
+
+@pytest.mark.parametrize("name", list(PATHS) + ["start_and_length_of_single_rows"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scan_rooms_and_prefixes(name, dtype):
+    batch = PATHS[name] if name in PATHS else rooms([1, 0, 1, 1, 0, 1], 2, 5)
+    for states, hook in ((16, 0), (13, 1), (16, 3), (16, 1 | 1 << 2), (13, 2 | 1 << 2), (3, 1 | 2 << 2)):
+        scan_case(batch, 22, states, 2, dtype, True, True, True, 1, states, scale=0.1, hook=hook)
+
+
+@pytest.mark.parametrize("layout", ["packed", "padded", "rooms"])
+@pytest.mark.parametrize("count,per_lane", [(20, 3), (41, 2), (63, 3), (64, 1), (64, 3)])
+def test_scan_longest_sequences_first(layout, count, per_lane):
+    """More than 256 workgroups and 32 rows a sequence on the average: sequences in the order of their lengths, equal and empty ones
+    among them.  `per_lane`: the hook for four, two or one of 16 states a lane, so 64, 32 or 16 channels a workgroup."""
+    width = {1: 64, 2: 32, 3: 16}[per_lane]
+    lengths = ragged(count, 38, count)
+    if layout == "padded":
+        batch = Batch(lengths, "padded", tail=1)
+    else:
+        lengths[-1] += max(0, 33 * count - sum(lengths))
+        batch = Batch(lengths, "packed", tail=2) if layout == "packed" else rooms(lengths, 3, count)
+    channels = width * (256 // count + 1)
+    assert batch.tokens // count >= 32 and channels // width * count > 256 and len(set(lengths)) < count
+    assert scan_case(batch, channels, 16, 1, "bf16", True, True, True, 0, count, scale=0.1, hook=per_lane) == 0
+
+
+@pytest.mark.parametrize("count", [65, 128, 129, 200])
+@pytest.mark.parametrize("layout", ["packed", "padded", "rooms"])
+def test_scan_pieces_of_many_sequences(count, layout):
+    """Pieces of 64 rows of more than 64 sequences, of no piece, one and several each."""
+    lengths = [n if n < 400 else 400 for n in ragged(count, 50, count + 1)]
+    if layout == "padded":
+        lengths = [min(n, 140) for n in lengths]
+    assert max(lengths) > 128 and 0 in lengths and 1 in lengths
+    batch = {"packed": lambda: Batch(lengths, "packed", tail=9, source=[(i * 3) % count for i in range(count)], target=[count + i for i in range(count)],
+                                     slots=2 * count),
+             "padded": lambda: Batch(lengths, "padded", tail=1), "rooms": lambda: rooms(lengths, 4, count)}[layout]()
+    for code, dtype in ((1, "bf16"), (3, "f32")):
+        assert scan_case(batch, 18, 16, 1, dtype, True, True, True, 0, count, scale=0.02, hook=code | 1 << 2) > 0
