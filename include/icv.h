@@ -380,8 +380,9 @@ ICV_API int icv_quantize_fp8(const icv_quantize_params* p, const void* input, vo
  * out[m][n] = bias[n] + sum over k of a[m][k] * b[n][k]: the pointwise convolution with rows of pixels a and the
  * filter b ([K][C], section 3.2's plain GEMM), both in the form above, a with block_rows 1, b with 128.  A block's sum
  * of 128 products is multiplied by the block's two scales and added to a float sum.  For a float output all of it is
- * float arithmetic; for a bfloat16 output a block's products are summed by the e4m3 instruction, which cuts each to 13
- * bits below the largest of its 8 neighbours (about 1.5e-5 of the result).  rows = 0: nothing to do, ICV_OK.
+ * float arithmetic; for a bfloat16 output a block's products are summed by the e4m3 instruction, 8 neighbours at a time,
+ * each of which loses less than 2^-13 of the largest of the 8: at most 7 * 2^-13 of the sum of |a * b| in all, where
+ * products cancel too, and about 1.5e-5 of the outputs' size over random operands.  rows = 0: nothing to do, ICV_OK.
  *   a, b  : 16-byte aligned; a_scales [ceil(depth/128)][rows], b_scales [ceil(depth/128)][ceil(cols/128)]
  *   bias  : cols floats or NULL
  *   out   : [rows] rows of out_row_stride elements, not over a or b: float (ICV_OUT_ACC) or bfloat16 (ICV_OUT_BF16)

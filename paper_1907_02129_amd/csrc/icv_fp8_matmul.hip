@@ -40,8 +40,9 @@ __device__ inline bf16x8_t widen(int lo, int hi)
 // the output, row l % 16.
 //
 // The e4m3 instruction adds 8 products at a time, each cut to 13 bits below the largest one's leading bit (measured:
-// 2^16 + 15 gives 2^16 + 8, in the same 8 only); the eights are added in float.  Over random operands that is 1.5e-5 of the
-// result, far below a bfloat16 output's rounding (2^-9) but not below a float's.  EXACT, for float outputs, widens the codes to bfloat16
+// 2^16 + 15 gives 2^16 + 8, in the same 8 only); the eights are added in float.  So 7 of 8 lose less than 2^-13 of the largest each, at
+// most 7 * 2^-13 of the sum of the products' sizes; over random operands 1.5e-5 of the outputs' size, far below a bfloat16 output's
+// rounding (2^-8) but not below a float's.  EXACT, for float outputs, widens the codes to bfloat16
 // (no rounding) and uses that type's instruction, whose products and sums are float's, at half the rate.
 template <bool EXACT>
 struct Operand;
@@ -144,12 +145,6 @@ __device__ inline void copy4_global_to_lds(const void* sbase, uint32_t voff, uin
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1\n" : : "v"(voff), "s"(sbase), "s"(lds_base) : "memory");
 }
 
-// BN columns x BM rows per workgroup of WN x WM wavefronts, each a grid of 16 x 16 blocks.  A stage holds one block of
-// 128 of the reduction: BN rows of b, BM rows of a (128 bytes each), their scales.  Two stages: one is multiplied while the
-// other is on its way.  A row's eight 16-byte pieces are stored permuted by the row's number, so that the rows that an
-// instruction's lanes read side by side lie in different banks; the permutation is made by the lanes' choice of
-// what to fetch.  A wavefront keeps its rows of a in registers for the stage and passes over its columns; a product is
-// scaled and added LAG instructions after its own, while those run.
 // A workgroup barrier behind this wavefront's LDS reads: what they read may be overwritten after it.  Copies to LDS that
 // are still on their way are not waited for.
 __device__ inline void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
@@ -162,6 +157,12 @@ constexpr int tile_pass_rows(int NW, int MW)
     return MW < most ? MW : most;
 }
 
+// BN columns x BM rows per workgroup of WN x WM wavefronts, each a grid of 16 x 16 blocks.  A stage holds one block of
+// 128 of the reduction: BN rows of b, BM rows of a (128 bytes each), their scales.  Two stages: one is multiplied while the
+// other is on its way.  A row's eight 16-byte pieces are stored permuted by the row's number, so that the rows that an
+// instruction's lanes read side by side lie in different banks; the permutation is made by the lanes' choice of
+// what to fetch.  A wavefront keeps its rows of a in registers for the stage and passes over its columns; a product is
+// scaled and added LAG instructions after its own, while those run.
 template <typename OUT, int BN, int BM, int WN, int WM, int KG, bool AHEAD>
 __global__ __launch_bounds__(64 * WN * WM * KG, 2) void k_matmul_tile(MatmulArgs g)
 {
