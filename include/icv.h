@@ -291,7 +291,8 @@ typedef struct icv_sequences {
 /*
  * Short causal convolution of every channel d along its sequence, t counted in the sequence:
  *   y[t][d] = act(bias[d] + sum_k filter[d][k] * x[t - (taps-1) + k][d]),  act(v) = v, or v / (1 + exp(-v)) with silu,
- * sums in float, one rounding at the store.  Rows in front of the first are the taps-1 rows of the state (oldest
+ * sums in float, one rounding at the store (a quotient under 2^-119 in size may come out as 0; so may the scan's, and a delta under
+ * 2^-126).  Rows in front of the first are the taps-1 rows of the state (oldest
  * first); the state behind a sequence is the last taps-1 rows of the old state and the sequence's own.
  *   input  : [tokens] rows of in_row_stride elements (first `channels` used)
  *   filter : [channels][taps], of the rows' type (Listing 1's filter for one channel in and out), bias: channels floats or NULL

@@ -54,9 +54,6 @@ __device__ inline int32_t seq_slot(const SeqArgs& s, const int32_t* which, int32
     return v >= 0 && v < s.slots ? v : -1;
 }
 
-template <typename T>
-__device__ inline float to_float(T v) { return (float)v; }
-
 // N elements from any address of the element's own alignment (one wide load: global memory takes any address),
 // `n` < N of them where a row ends; the rest read as zero.
 template <int N, typename T>
@@ -142,8 +139,8 @@ struct Raw {
     }
 };
 
-// v / (1 + exp(-v)).  exp(-v) overflows to infinity below -88, which gives -0, the limit; the reciprocal is the
-// hardware's, within 1 ulp, next to an output rounding of at least that.
+// v / (1 + exp(-v)).  The reciprocal is the hardware's, within 1 ulp, next to an output rounding of at least that; it has no
+// denormals, so below -87.3, where the quotient is under 2^-119 in size, it is -0, as where exp(-v) overflows.
 __device__ inline float silu(float v) { return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f)); }
 
 }  // namespace icv

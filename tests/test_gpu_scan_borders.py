@@ -90,3 +90,30 @@ def test_decays_over_a_piece_past_the_range_of_float(cut):
     assert want.isfinite().all() and bound.isfinite().all()
     ref.check("out", out, want, bound)
     ref.check("state", st, st_want, sbound)
+
+
+@pytest.mark.parametrize("step", [True, False])
+def test_activations_over_their_whole_range(step):
+    """log(1 + exp(v)) (the state after one row from zeros), v / (1 + exp(-v)) as the scan's gate and as the convolution's
+    activation, from -200 to 200 and next to 0, where results under 2^-126 and 2^-119 may be 0."""
+    v = torch.cat([torch.linspace(-200, 200, 3201), torch.exp2(torch.arange(-126.0, 1)), -torch.exp2(torch.arange(-126.0, 1))])
+    ch = len(v)
+    one, z = torch.ones(1, ch), v[None]
+    A, B, zeros = torch.zeros(ch, 1), torch.ones(1, 1), torch.zeros(1, ch, 1)
+    p = icv.make_scan_params(ch, 1, "f32", state_slots=1)
+    st, out = zeros.cuda(), torch.zeros(1, ch, device="cuda")
+    seq = icv.make_sequences(1, 1, None if step else ints([0, 1]))
+    assert icv.selective_scan_workspace_bytes(p, seq) == 0
+    icv.selective_scan(p, seq, one.cuda(), z.cuda(), A.cuda(), B.cuda(), B.cuda(), None, None, None, st, out)
+    want, bound, st_want, sbound = ref.selective_scan(one, z, A, B, B, None, None, None, zeros, [(0, 1)], [0], [0], 1, True, torch.zeros(1, ch),
+                                                      torch.float32)
+    ref.check("state", st, st_want, sbound + 2.0 ** -126)
+    ref.check("out", out, want, bound + 2.0 ** -126)
+    p = icv.make_scan_params(ch, 1, "f32", softplus=False)
+    icv.selective_scan(p, seq, one.cuda(), one.cuda(), A.cuda(), B.cuda(), B.cuda(), None, z.cuda(), None, None, out)
+    want, bound, _, _ = ref.selective_scan(one, one, A, B, B, None, z, None, zeros, [(0, 1)], [-1], [-1], 1, False, torch.zeros(1, ch), torch.float32)
+    ref.check("gate", out, want, bound + 2.0 ** -119)
+    filt = torch.ones(ch, 1)
+    icv.causal_conv1d(icv.make_causal_conv_params(ch, 1, "f32"), seq, z.cuda(), filt.cuda(), None, None, out)
+    want, bound, _ = ref.causal_conv(z, filt, None, torch.zeros(1, 0, ch), [(0, 1)], [-1], [-1], True, torch.zeros(1, ch), torch.float32)
+    ref.check("activation", out, want, bound + 2.0 ** -119)
