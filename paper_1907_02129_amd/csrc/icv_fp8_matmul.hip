@@ -6,7 +6,7 @@
 // the 4 outputs that a lane holds, which are neighbouring columns of one row).
 //
 // 12288 x 8192, 4096 deep to bfloat16: 390 us, 2.1 PFLOP/s (the vendor's product without block scales: 346; with operands of zeros 351,
-// the difference being power); to float 735.  8 x 4096, 2048 deep: 4.8 us, a launch; 8 x 4096, 8192 deep 10.6, 3.2 TB/s of filter;
+// the difference being power); to float 735.  8 x 4096, 2048 deep: 4.1 us, a launch; 8 x 4096, 8192 deep 10.6, 3.2 TB/s of filter;
 // 64 x 8192, 4096 deep 11.5; 2048 x 4096, 4096 deep 41, 1.7 PFLOP/s.
 #include "icv_mfma_common.h"
 #include "icv_sequence.h"
@@ -91,8 +91,8 @@ __device__ inline void store_out(const MatmulArgs& g, int64_t m, int32_t n, f32x
 }
 
 // 16 columns x 16 rows per workgroup, the blocks of the reduction dealt to its wavefronts, whose sums meet in LDS.
-// For few rows, where reading b is all there is: a wavefront has the codes of two blocks on their way at once (four: 8 x 4096,
-// 2048 deep 6.0 us instead of 5.9).
+// For few rows, where reading b is all there is: a wavefront has the codes of two blocks on their way at once (8 x 4096, 2048
+// deep 4.1 us, and the same with four).
 template <typename OUT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void k_matmul_split(MatmulArgs g)
 {
