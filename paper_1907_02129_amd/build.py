@@ -4,13 +4,16 @@
 
 Every .hip file under csrc/ is compiled to an object (in parallel) and linked into
 paper_1907_02129_amd/libicv.so.  hipcc cross-compiles without a GPU present.  The host compiler builds
-icv_python.cpp, the argument checks of the operators that take torch tensors, into _icv_python.so beside it.
+icv_python.cpp, the argument checks of the operators that take torch tensors, into _icv_python.so beside it; libicv.so needs
+neither, and is built without it where torch, Python's headers or that compiler are missing.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
 import glob
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
 import sysconfig
@@ -50,6 +53,19 @@ def _compile(src: str, verbose: bool, incremental: bool = False) -> str:
     return obj
 
 
+def missing_for_python_module() -> str:
+    """What is not there of the things that only _icv_python.so needs; "" if all are."""
+    torch = importlib.util.find_spec("torch")
+    if torch is None or not torch.origin:
+        return "torch"
+    if not os.path.exists(os.path.join(os.path.dirname(torch.origin), "include", "torch", "csrc", "autograd", "python_variable.h")):
+        return "torch's headers"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h"
+    cxx = os.environ.get("CXX", "g++")
+    return "" if shutil.which(cxx) else cxx
+
+
 def build_python_module(verbose: bool = False, incremental: bool = False) -> str:
     import torch                                  # its headers and libraries; the module runs in a process that has torch loaded
     src, at = os.path.join(CSRC, "icv_python.cpp"), os.path.dirname(os.path.abspath(torch.__file__))
@@ -74,14 +90,22 @@ def build(verbose: bool = False, jobs: int = 8, incremental: bool = False) -> st
     """Compile every source (or, with `incremental`, those newer than their object) and link the library."""
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    missing = missing_for_python_module()
     with cf.ThreadPoolExecutor(max_workers=min(jobs, len(srcs) + 1)) as ex:
-        module = ex.submit(build_python_module, verbose, incremental)
+        module = None if missing else ex.submit(build_python_module, verbose, incremental)
         objs = list(ex.map(lambda s: _compile(s, verbose, incremental), srcs))
-        module.result()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.run(cmd, check=True)
+    if module:
+        module.result()
+    else:
+        # an old one would check against another description of the structs
+        if os.path.exists(PYTHON_MODULE):
+            os.remove(PYTHON_MODULE)
+        print(f"without _icv_python.so, which needs {missing}: the library's C interface is complete, the operators on sequences and in "
+              "8-bit floating point cannot be called through binding.py", file=sys.stderr)
     return LIB
 
 
