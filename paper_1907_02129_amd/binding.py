@@ -349,6 +349,8 @@ def _indices(name, t, n, device):
     """Address of a contiguous int32 tensor of at least n elements; None for none."""
     if t is None:
         return None
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: a tensor expected, got {type(t)}")
     if t.dtype is not torch.int32 or t.get_device() != device or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous int32 tensor of at least {n} elements, all such on one GPU, expected")
     return t.data_ptr()
@@ -358,7 +360,7 @@ def make_sequences(count, tokens, start=None, length=None, from_slot=None, to_sl
     """icv_sequences; the arrays are int32 device tensors, kept alive by the result.  `start` has count + 1 entries, the
     others count; what they hold is read when the kernels run."""
     arrays = tuple(t for t in (start, length, from_slot, to_slot) if t is not None)
-    device = arrays[0].get_device() if arrays else -1
+    device = next((t.get_device() for t in arrays if isinstance(t, torch.Tensor)), 0 if arrays else -1)       # others are refused below
     if arrays and device < 0:
         raise ValueError("icv takes device tensors")
     s = icv_sequences(count, tokens, _indices("start", start, count + 1, device), _indices("length", length, count, device),

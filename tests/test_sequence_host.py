@@ -238,3 +238,12 @@ def test_rows_per_run_that_no_convolution_has(lib):
     for hook in (33, 64, 1 << 20):                                                      # test hooks
         assert conv(lib, silu=1 | hook << 8) == UNSUPPORTED
     assert conv(lib, silu=-1) == BAD and conv(lib, silu=4 << 8 | 2) == BAD
+
+
+@pytest.mark.parametrize("name", ["start", "length", "from_slot", "to_slot"])
+def test_sequences_of_something_else_than_tensors_are_a_type_error(name):
+    for wrong in ([0, 4], 0, "0"):
+        with pytest.raises(TypeError, match=name + ": a tensor expected"):
+            icv.make_sequences(1, 4, **{name: wrong})
+    with pytest.raises(ValueError, match="device tensors"):
+        icv.make_sequences(1, 4, start=[0, 4], length=torch.zeros(1, dtype=torch.int32))
