@@ -149,6 +149,13 @@ __device__ inline void copy4_global_to_lds(const void* sbase, uint32_t voff, uin
 // are still on their way are not waited for.
 __device__ inline void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
+// Accesses to LDS before and after this stay so: lanes of one wavefront hand values to each other.  No instruction.
+__device__ inline void lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Rows of a wavefront's MW x NW outputs that its part of LDS takes at a time.
 template <typename OUT>
 constexpr int tile_pass_rows(int NW, int MW)
@@ -357,6 +364,8 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void k_matmul_tile(MatmulArgs
                 for (int r = 0; r < 4; r++) o[r] = (OUT)(v[r] + bias[r]);
             }
         }
+        // the other lanes' part of the region: LDS serves a wavefront in its order, which the compiler has to keep
+        lds_order();
         const int c = (lane % LPR) * V;
 #pragma unroll
         for (int r = 0; r < RP; r += 64 / LPR) {
@@ -373,6 +382,7 @@ __global__ __launch_bounds__(64 * WN * WM * KG, 2) void k_matmul_tile(MatmulArgs
                 }
             }
         }
+        lds_order();
     }
 }
 
