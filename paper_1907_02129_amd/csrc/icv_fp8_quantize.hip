@@ -37,8 +37,9 @@ __device__ inline float scale_of(float most)
 // Quotients by a scale, rounded correctly as the definition says.  For scales far from the ends of float's range:
 // with r the rounded reciprocal, q = v * r and one correction by the exact remainder, q + (v - q * scale) * r, is the rounded
 // quotient (Markstein's theorem), in three operations; the division that takes every case has eleven (12288 x 4096 bfloat16, four rows a wavefront: 43.4 us, 35.6 with
-// this).  The step from the hardware's reciprocal to r rounds correctly except, as the theorem goes, for a significand of all
-// ones, where r is right if the hardware's value was; that it is there is among the tests (elsewhere powers of two over it next to a tie would go wrong).
+// this).  The step from the hardware's reciprocal to r rounds correctly for every significand but one of all ones (24 bits).
+// There r is right if the hardware's value is, which a test shows; otherwise a power of two over such a scale, next to a
+// tie between two codes, would be rounded to the wrong side.
 struct Divider {
     float scale, r;
     bool plain;
